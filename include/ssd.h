@@ -1,6 +1,7 @@
 /*
  * ssd.h -- C ABI of the MI355X (gfx950) SSD layer: forward, decode step,
- * block steps, span state passing, and gradients.
+ * block steps, span state passing, and gradients; and of what stands around it
+ * in a block: short convolution, selective scan, residual addition with norm.
  *
  * Computes y = SSM(A, B, C)(x) for the scalar-transition selective SSM of the
  * SSD layer (Section 5 of "Transformers are SSMs"), by the chunked block
@@ -465,6 +466,179 @@ int ssd_forward_noalloc(const ssd_problem* prob,
                         const void* B, const void* C, const float* D,
                         const float* initial_states, const int32_t* seq_idx,
                         void* y, float* final_states, int32_t* status, void* stream);
+
+/* ---- The short convolution in front of the layer -----------------------------
+ *
+ * The block's causal depthwise convolution over `width` tokens, with SiLU:
+ *     v_t,c = bias_c + sum_{j < width} weight_c,j x_{t - width + 1 + j, c}
+ *     y_t,c = v_t,c sigmoid(v_t,c)      (silu != 0; else y = v)
+ * The rows before a sequence's first token are its initial state (zero when
+ * NULL), the last width - 1 inputs of what came before, oldest first; its final
+ * state is the last width - 1 rows of (initial state, inputs).
+ *
+ * Layouts (last dimension contiguous):
+ *   x               (batch, seqlen, channels) dtype, element strides
+ *                   x_batch_stride and x_token_stride (>= 0): it may be a slice
+ *                   of a wider projection's output
+ *   y, dy           nparts tensors (batch, seqlen, parts[i]) dtype, contiguous:
+ *                   the channels in order, cut into 1 to 3 parts that add up to
+ *                   `channels` (x, B and C of the layer, say).  y and dy are host
+ *                   arrays of nparts device pointers, read during the call
+ *   weight          (channels, width) float32;  bias (channels) float32 or NULL
+ *   seq_idx         (1, seqlen) int32 or NULL: one packed row of nseq sequences
+ *                   (the contract of ssd_forward; ids that break it give
+ *                   unspecified values but no access outside the buffers)
+ *   initial_states, final_states
+ *                   (batch, width - 1, channels) dtype, contiguous, or NULL;
+ *                   (nseq, width - 1, channels) with seq_idx
+ * Arithmetic in float32; results are rounded to dtype once (nearest even).
+ * 2 <= width <= 4 (else SSD_ERR_UNSUPPORTED_DIMS).  Outputs must not overlap
+ * inputs.  Ownership, asynchrony, determinism and errors as for ssd_forward. */
+typedef struct {
+    int64_t batch, seqlen, channels, width;
+    int64_t nseq;             /* read only when seq_idx != NULL                  */
+    int64_t x_batch_stride;   /* elements between batch rows of x                */
+    int64_t x_token_stride;   /* elements between tokens of x                    */
+    int64_t nparts;           /* 1 to 3                                          */
+    int64_t parts[3];         /* channels of each part, in order                 */
+    int32_t dtype;            /* ssd_dtype of x, y and the states                */
+    int32_t silu;
+} ssd_conv_problem;
+
+int ssd_conv_forward(const ssd_conv_problem* prob, const void* x, const float* weight, const float* bias,
+                     const void* initial_states, const int32_t* seq_idx, void* const* y, void* final_states,
+                     void* stream);
+
+/* Gradients of ssd_conv_forward, given dy (in the same parts) and dfinal_states
+ * (NULL = 0).  Every output is overwritten: dx (batch, seqlen, channels) dtype,
+ * contiguous; dweight (channels, width) and dbias (channels) float32 (dbias may
+ * be NULL); dinitial_states as initial_states, dtype, may be NULL.  Workspace:
+ * ssd_conv_backward_workspace_bytes(). */
+int ssd_conv_backward_workspace_bytes(const ssd_conv_problem* prob, size_t* bytes);
+
+int ssd_conv_backward(const ssd_conv_problem* prob, const void* x, const float* weight, const float* bias,
+                      const void* initial_states, const int32_t* seq_idx, const void* const* dy,
+                      const void* dfinal_states, void* dx, float* dweight, float* dbias, void* dinitial_states,
+                      void* workspace, size_t workspace_bytes, void* stream);
+
+/* One token per sequence: x (batch, channels) with x_batch_stride between rows,
+ * y (batch, channels) contiguous, state (batch, width - 1, channels) dtype, read
+ * and moved on by one token in place.  seqlen, nseq, x_token_stride and the
+ * parts are ignored. */
+int ssd_conv_step(const ssd_conv_problem* prob, const void* x, const float* weight, const float* bias, void* state,
+                  void* y, void* stream);
+
+/* ---- The selective scan ------------------------------------------------------
+ *
+ * The layer of the first kind of Mamba block: a diagonal state space model with a
+ * decay of its own for every channel e and state n (the scalar-transition layer
+ * above has one decay per head).  Group g = e / (channels / ngroups):
+ *     dt_t,e = softplus(dt_in_t,e + dt_bias_e)     (dt_softplus == 0: without softplus)
+ *     h_t,e,n = exp(dt_t,e A_e,n) h_{t-1},e,n + dt_t,e x_t,e B_t,g,n,  A = -exp(A_log)
+ *     y_t,e = sum_n h_t,e,n C_t,g,n + D_e x_t,e,   times z_t,e sigmoid(z_t,e) when z
+ * Layouts (last dimension contiguous; element strides >= 0 between batch rows and
+ * between tokens where the problem has them, so that x, dt, z, B and C may be
+ * slices of wider tensors):
+ *   x, dt, z        (batch, seqlen, channels) dtype; z may be NULL
+ *   B, C            (batch, seqlen, ngroups, dstate) dtype, groups contiguous;
+ *                   4-byte aligned with even strides (else SSD_ERR_UNSUPPORTED_DIMS)
+ *   A_log           (channels, dstate) float32
+ *   D, dt_bias      (channels) float32, may be NULL (= 0)
+ *   y, dy           (batch, seqlen, channels) dtype, contiguous
+ *   seq_idx         (1, seqlen) int32 or NULL: one packed row of nseq sequences
+ *   initial_states, final_states   (batch, channels, dstate) float32, 16-byte
+ *                   aligned, contiguous, or NULL; (nseq, ...) with seq_idx
+ * dstate is a multiple of 16 in [16, 256].  The states and all arithmetic are
+ * float32; a decay below 2^-126 counts as 0.  The sequence is cut into chunks
+ * where its channels alone do not fill the device: their states from zero, a scan
+ * over the chunks, then the outputs.  Workspace: ssd_scan_workspace_bytes() (for
+ * the forward; may be 0).  Ownership, asynchrony, determinism and errors as for
+ * ssd_forward. */
+typedef struct {
+    int64_t batch, seqlen, channels, dstate, ngroups;
+    int64_t nseq;                             /* read only when seq_idx != NULL      */
+    int64_t x_batch_stride, x_token_stride;   /* elements                            */
+    int64_t dt_batch_stride, dt_token_stride;
+    int64_t z_batch_stride, z_token_stride;
+    int64_t b_batch_stride, b_token_stride;
+    int64_t c_batch_stride, c_token_stride;
+    int32_t dtype;                            /* ssd_dtype of x, dt, z, B, C, y      */
+    int32_t dt_softplus;
+} ssd_scan_problem;
+
+int ssd_scan_workspace_bytes(const ssd_scan_problem* prob, size_t* bytes);
+
+int ssd_scan_forward(const ssd_scan_problem* prob, const void* x, const void* dt, const float* A_log,
+                     const void* B, const void* C, const float* D, const void* z, const float* dt_bias,
+                     const float* initial_states, const int32_t* seq_idx, void* y, float* final_states,
+                     void* workspace, size_t workspace_bytes, void* stream);
+
+/* Gradients of ssd_scan_forward, given dy and dfinal_states (NULL = 0).  Every
+ * output is overwritten: dx, ddt (of dt_in, before bias and softplus), dz
+ * (required with z) like y; dB, dC (batch, seqlen, ngroups, dstate) dtype,
+ * contiguous; dA_log (channels, dstate) float32; dD and ddt_bias (channels)
+ * float32, written when not NULL and the input is given; dinitial_states like
+ * initial_states, may be NULL.  The states are computed again from the inputs.
+ * Workspace: ssd_scan_backward_workspace_bytes(). */
+int ssd_scan_backward_workspace_bytes(const ssd_scan_problem* prob, size_t* bytes);
+
+int ssd_scan_backward(const ssd_scan_problem* prob, const void* x, const void* dt, const float* A_log,
+                      const void* B, const void* C, const float* D, const void* z, const float* dt_bias,
+                      const float* initial_states, const int32_t* seq_idx, const void* dy,
+                      const float* dfinal_states, void* dx, void* ddt, float* dA_log, void* dB, void* dC,
+                      float* dD, void* dz, float* ddt_bias, float* dinitial_states,
+                      void* workspace, size_t workspace_bytes, void* stream);
+
+/* One token per sequence: x, dt, z (batch, channels), B, C (batch, ngroups,
+ * dstate) with the batch strides of the problem (seqlen, nseq and token strides
+ * are ignored; no alignment beyond their type's), y (batch, channels) contiguous,
+ * state (batch, channels, dstate) float32, 16-byte aligned, updated in place. */
+int ssd_scan_step(const ssd_scan_problem* prob, const void* x, const void* dt, const float* A_log,
+                  const void* B, const void* C, const float* D, const void* z, const float* dt_bias,
+                  float* state, void* y, void* stream);
+
+/* ---- Residual addition and RMS norm between blocks ---------------------------
+ *
+ * Per row of `channels` values, r = x + residual (residual NULL = 0), in float32:
+ *     residual_out = r rounded to residual_dtype           (NULL: not written)
+ *     y = r / sqrt(mean(r^2) + eps) * weight               (weight NULL = 1)
+ * from the unrounded r.  out_dtype says what y is:
+ *   SSD_DTYPE_F32, SSD_DTYPE_BF16   y itself, which has x's dtype
+ *   SSD_DTYPE_I8, SSD_DTYPE_E4M3    8-bit values q with a scale per row, y ~ q scale:
+ *       t = r weight, m = max |t|, q = (t / m) top rounded to nearest even,
+ *       scale = m / sqrt(mean(r^2) + eps) / top, top = 127 (I8) or 448 (E4M3, the
+ *       format with no infinities).  A row of zeros has scale 0 and q 0; a row
+ *       that holds a NaN or an infinity, or whose squares overflow float32, has
+ *       scale NaN and q 0.
+ * x, residual, y, residual_out are contiguous (rows, channels); x's dtype is
+ * `dtype`, the residual's residual_dtype (float32 where x is).  weight (channels)
+ * float32.  1 <= channels <= 32768 (else SSD_ERR_UNSUPPORTED_DIMS).  residual_out may be residual itself (in
+ * place); otherwise outputs must not overlap inputs. */
+enum { SSD_DTYPE_I8 = 2, SSD_DTYPE_E4M3 = 3 };
+
+typedef struct {
+    int64_t rows, channels;
+    int32_t dtype;            /* ssd_dtype of x (and dy, dx)       */
+    int32_t residual_dtype;   /* ssd_dtype of the residual         */
+    int32_t out_dtype;        /* of y: dtype, SSD_DTYPE_I8 or _E4M3 */
+    float eps;                /* >= 0 and finite                   */
+} ssd_norm_problem;
+
+/* `scale` (rows) float32 is written with the 8-bit types (NULL otherwise). */
+int ssd_add_norm(const ssd_norm_problem* prob, const void* x, const void* residual, const float* weight, void* y,
+                 float* scale, void* residual_out, void* stream);
+
+/* Gradients, given `residual` = the forward's residual_out (r, in
+ * residual_dtype), dy (dtype) and dresidual_out (residual_dtype, NULL = 0): the
+ * gradient of r, which is that of x and that of the residual, rounded to dtype
+ * in dx and to residual_dtype in dresidual (either may be NULL, not both);
+ * dweight (channels) float32, may be NULL.  out_dtype is ignored.  Workspace:
+ * ssd_add_norm_backward_workspace_bytes(). */
+int ssd_add_norm_backward_workspace_bytes(const ssd_norm_problem* prob, size_t* bytes);
+
+int ssd_add_norm_backward(const ssd_norm_problem* prob, const void* dy, const void* residual, const float* weight,
+                          const void* dresidual_out, void* dx, void* dresidual, float* dweight,
+                          void* workspace, size_t workspace_bytes, void* stream);
 
 /* Static, NUL-terminated description of a status code. */
 const char* ssd_error_string(int code);

@@ -1,0 +1,193 @@
+// Internal interface and device helpers of the operators around the layer: the
+// short convolution (ssd_conv.hip), the selective scan (ssd_scan.hip,
+// ssd_scan_bwd.hip) and the residual addition with norm (ssd_norm.hip).
+// Host validation: ssd_ops_api.cpp.
+#pragma once
+
+#include "ssd_device.h"
+
+namespace ssd {
+
+// ---- parameters ------------------------------------------------------------
+
+struct ConvParams {
+    int64_t b, T, C, nseq;
+    int W, silu, nparts;
+    int64_t off[4];         // first channel of each part, then C
+    const void* x;
+    int64_t xb, xt;         // element strides of batch rows and tokens
+    const float* weight;    // (C, W)
+    const float* bias;      // (C) or null
+    const void* init;       // (units, W - 1, C) or null
+    const int32_t* seq_idx; // (T) or null
+    void* y[3];             // step: y[0]
+    void* fin;              // (units, W - 1, C) or null; step: the state
+    // gradients
+    const void* dy[3];
+    const void* dfin;
+    void* dx;
+    void* dinit;
+    float* dweight;
+    float* dbias;
+    float* partial;         // workspace: (strips, W + 1, C)
+};
+
+// Tokens per strip of the gradient kernel, and its workspace.
+int64_t conv_bwd_strip(int64_t b, int64_t T, int64_t C);
+hipError_t launch_conv_forward(const ConvParams& p, bool bf16, hipStream_t stream);
+hipError_t launch_conv_backward(const ConvParams& p, bool bf16, hipStream_t stream);
+hipError_t launch_conv_step(const ConvParams& p, bool bf16, hipStream_t stream);
+
+struct ScanParams {
+    int64_t b, T, E, N, G, nseq;
+    const void *x, *dt, *z, *B, *C;      // z may be null
+    int64_t xb, xt, db, dtt, zb, zt, bb, bt, cb, ct;   // element strides: batch row, token
+    const float *A_log, *D, *dt_bias;    // D, dt_bias may be null
+    const float* init;                   // (units, E, N) or null
+    const int32_t* seq_idx;
+    void* y;
+    float* fin;                          // or null; step: the state
+    int softplus;
+    // time split: S chunks of L tokens (S == 1: none), a workspace of chunk
+    // states (b, S, N, E) and of each chunk's sum of dt (b, S, E)
+    int64_t S, L;
+    float* states;
+    float* sums;
+    // gradients
+    const void* dy;
+    const float* dfin;
+    void *dx, *ddt, *dB, *dC, *dz;
+    float *dA_log, *dD, *ddt_bias, *dinit;
+    float* rstates;                      // (b, S, N, E) reverse chunk states
+    float* marks;                        // states at every kBwdTile tokens (b, tiles, N, E)
+    float* pA;                           // (b S, N, E) partial sums of dA
+    float* pD;                           // (b S, 2, E) of dD, ddt_bias
+    float* pBC;                          // (channel blocks, b, T, 2, N) of dB, dC
+};
+
+struct ScanPlan {
+    int64_t S, L;
+    size_t states, sums, rstates, marks, pA, pD, pBC, total;   // byte offsets
+    int64_t cblocks;   // channel blocks of the gradients
+};
+
+ScanPlan scan_plan(int64_t b, int64_t T, int64_t E, int64_t N, int64_t G, bool backward);
+hipError_t launch_scan_forward(const ScanParams& p, bool bf16, hipStream_t stream);
+hipError_t launch_scan_backward(const ScanParams& p, bool bf16, hipStream_t stream);
+hipError_t launch_scan_step(const ScanParams& p, bool bf16, hipStream_t stream);
+
+struct NormParams {
+    int64_t rows, C;
+    float eps;
+    const void* x;         // gradients: dy
+    const void* res;       // or null; gradients: r
+    const float* weight;   // or null
+    void* y;               // gradients: dx
+    float* scale;
+    void* res_out;         // or null; gradients: dresidual
+    const void* dres;      // gradients: dresidual_out, or null
+    float* dweight;
+    float* partial;
+};
+
+enum NormOut { kNormSame = 0, kNormI8, kNormE4M3 };
+// Workgroups' partial rows of dweight in the gradient kernel.
+int64_t norm_bwd_partials(int64_t rows, int64_t C);
+hipError_t launch_add_norm(const NormParams& p, bool bf16, bool res_bf16, NormOut out, hipStream_t stream);
+hipError_t launch_add_norm_backward(const NormParams& p, bool bf16, bool res_bf16, hipStream_t stream);
+
+// Most workgroups of one launch (grid x, with room for its thread count in 32 bits).
+constexpr int64_t kMaxGrid = 0x7fffffffLL / 1024;
+
+#if defined(__HIP_DEVICE_COMPILE__) || defined(__HIPCC__)
+
+// ---- device helpers ----------------------------------------------------------
+
+// Loads through the scalar cache: a uniform address of memory that the kernel
+// does not write.
+template <typename T>
+__device__ __forceinline__ T scalar_load(const T* p)
+{
+    return *reinterpret_cast<const __attribute__((address_space(4))) T*>(reinterpret_cast<uintptr_t>(p));
+}
+
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// A sequence id held to the states' range.
+__device__ __forceinline__ int64_t held(int32_t id, int64_t nseq)
+{
+    const int64_t v = id < 0 ? 0 : id;
+    return v < nseq ? v : nseq - 1;
+}
+
+// exp(-v) with the exponent's rounding error put back (a relative error near
+// 2e-7 for every v, where exp2(-v log2(e)) alone is off by |v| 6e-8); v is held
+// to +-104, beyond which the result is infinite or 0.
+__device__ __forceinline__ float exp_neg(float v)
+{
+    constexpr float kLog2eLow = 1.4426950408889634 - 1.44269502162933349609375;
+    v = -__builtin_amdgcn_fmed3f(v, -104.f, 104.f);
+    const float t = v * kLog2e;
+    const float low = fmaf(v, kLog2e, -t) + v * kLog2eLow;
+    const float e = __builtin_amdgcn_exp2f(t);
+    return fmaf(e, low * 0.69314718f, e);
+}
+
+__device__ __forceinline__ float sigmoid_hw(float v) { return __builtin_amdgcn_rcpf(1.f + exp_neg(v)); }
+
+// softplus(v) = max(v, 0) + log(1 + u), u = exp(-|v|) in (0, 1]: log(1 + u) =
+// 2 atanh(s), s = u / (2 + u) <= 1/3, by its power series up to s^15 (the next
+// term is 3e-9 of the sum).  Relative error near 2e-7 also where the result is
+// as small as u, as a time step is.
+__device__ __forceinline__ float softplus_hw(float v)
+{
+    const float u = exp_neg(fabsf(v));
+    const float s = u * __builtin_amdgcn_rcpf(2.f + u), q = s * s;
+    float r = fmaf(q, 1.f / 15, 1.f / 13);
+    r = fmaf(r, q, 1.f / 11);
+    r = fmaf(r, q, 1.f / 9);
+    r = fmaf(r, q, 1.f / 7);
+    r = fmaf(r, q, 1.f / 5);
+    r = fmaf(r, q, 1.f / 3);
+    r = fmaf(r, q, 1.f);
+    // (a NaN stays one: fmaxf drops it, the comparison does not)
+    return fmaf(2.f * s, r, v > 0.f ? v : v < 0.f ? 0.f : v);
+}
+
+__device__ __forceinline__ float widen(float v) { return v; }
+__device__ __forceinline__ float widen(uint16_t v) { return __uint_as_float(static_cast<uint32_t>(v) << 16); }
+
+template <typename T>
+__device__ __forceinline__ T narrow(float v);
+template <>
+__device__ __forceinline__ float narrow<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ uint16_t narrow<uint16_t>(float v)   // round to nearest even
+{
+    return __builtin_bit_cast(uint16_t, static_cast<__bf16>(v));
+}
+
+// V consecutive values of T at any alignment that T itself has (the hardware
+// reads and writes vectors at any).
+template <typename T, int V>
+struct Pack {
+    typedef T vec __attribute__((ext_vector_type(V), aligned(sizeof(T))));
+    vec v;
+    __device__ __forceinline__ float operator[](int i) const { return widen(static_cast<T>(v[i])); }
+    __device__ __forceinline__ void set(int i, float f) { v[i] = narrow<T>(f); }
+    static __device__ __forceinline__ Pack load(const T* p) { return Pack{*reinterpret_cast<const vec*>(p)}; }
+    __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<vec*>(p) = v; }
+};
+
+template <typename T>
+struct Pack<T, 1> {
+    T v;
+    __device__ __forceinline__ float operator[](int) const { return widen(v); }
+    __device__ __forceinline__ void set(int, float f) { v = narrow<T>(f); }
+    static __device__ __forceinline__ Pack load(const T* p) { return Pack{*p}; }
+    __device__ __forceinline__ void store(T* p) const { *p = v; }
+};
+
+#endif
+
+}  // namespace ssd

@@ -1,0 +1,124 @@
+// Device pieces that the selective scan's forward (ssd_scan.hip) and gradients
+// (ssd_scan_bwd.hip) share.
+//
+// A lane holds a channel and a wavefront 64 of them, so that B_t and C_t, which
+// all channels of a group share, are uniform: they come through the scalar cache
+// into scalar registers, and every product with them takes one operand from there
+// (no shared memory, no sum across lanes for y).  A lane holds 16 states of its
+// channel in registers; more states take more wavefronts.
+#pragma once
+
+#include "ssd_ops.h"
+
+namespace ssd {
+
+constexpr int kSlice = 16;     // states a lane holds
+constexpr int kTok = 8;        // tokens whose loads are issued together
+constexpr int kBwdTile = 16;   // tokens per tile of the gradients
+
+// A wavefront's place: channel tile (64 channels of one group), chunk, batch row.
+struct ScanWork {
+    int64_t row, chunk, t0, t1;
+    int64_t g, e;      // group, the lane's channel (a lane past its group's end: the last one)
+    int64_t tile;      // channel tile within the group
+    bool live;
+};
+
+__host__ __device__ __forceinline__ int64_t scan_tiles(int64_t E, int64_t G) { return (E / G + 63) / 64; }
+
+__device__ __forceinline__ ScanWork scan_work(const ScanParams& p, int64_t unit)
+{
+    ScanWork w;
+    const int64_t per = scan_tiles(p.E, p.G), all = per * p.G, eg = p.E / p.G;
+    const int64_t at = unit / all, tile = unit - at * all;
+    w.row = at / p.S;
+    w.chunk = at - w.row * p.S;
+    w.t0 = w.chunk * p.L;
+    w.t1 = w.t0 + p.L < p.T ? w.t0 + p.L : p.T;
+    w.g = tile / per;
+    w.tile = tile - w.g * per;
+    const int64_t e = w.tile * 64 + (threadIdx.x & 63);
+    w.live = e < eg;
+    w.e = w.g * eg + (w.live ? e : eg - 1);
+    return w;
+}
+
+template <bool PACKED>
+__device__ __forceinline__ int64_t scan_unit(const ScanParams& p, int64_t row, int64_t t)
+{
+    if constexpr (!PACKED) return row;
+    return held(scalar_load(p.seq_idx + t), p.nseq);
+}
+
+// Whether token t > 0 starts a sequence / token t ends one.
+template <bool PACKED>
+__device__ __forceinline__ bool scan_starts(const ScanParams& p, int64_t t)
+{
+    if (t == 0) return true;
+    if constexpr (!PACKED) return false;
+    return scalar_load(p.seq_idx + t) != scalar_load(p.seq_idx + t - 1);
+}
+
+template <bool PACKED>
+__device__ __forceinline__ bool scan_ends(const ScanParams& p, int64_t t)
+{
+    if (t == p.T - 1) return true;
+    if constexpr (!PACKED) return false;
+    return scalar_load(p.seq_idx + t) != scalar_load(p.seq_idx + t + 1);
+}
+
+// K uniform values at a 4-byte aligned address, through the scalar cache.
+template <typename T, int K>
+__device__ __forceinline__ void uniform_row(const T* at, float (&v)[K])
+{
+    constexpr int D = K * sizeof(T) / 4;
+    typedef uint32_t words __attribute__((ext_vector_type(D), aligned(4)));
+    const words w = *reinterpret_cast<const __attribute__((address_space(4))) words*>(reinterpret_cast<uintptr_t>(at));
+#pragma unroll
+    for (int i = 0; i < D; ++i) {
+        if constexpr (sizeof(T) == 4) {
+            v[i] = __uint_as_float(w[i]);
+        } else {
+            v[2 * i] = __uint_as_float(w[i] << 16);
+            v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+        }
+    }
+}
+
+// A lane's 16 states of a unit, in the caller's layout (units, E, N).
+__device__ __forceinline__ void load_states(const float* s, const ScanParams& p, int64_t unit, int64_t e, int n0,
+                                            float (&h)[kSlice])
+{
+    if (!s) {
+#pragma unroll
+        for (int n = 0; n < kSlice; ++n) h[n] = 0.f;
+        return;
+    }
+    const float4* at = reinterpret_cast<const float4*>(s + (unit * p.E + e) * p.N + n0);
+#pragma unroll
+    for (int k = 0; k < kSlice / 4; ++k) {
+        const float4 v = at[k];
+        h[4 * k] = v.x;
+        h[4 * k + 1] = v.y;
+        h[4 * k + 2] = v.z;
+        h[4 * k + 3] = v.w;
+    }
+}
+
+__device__ __forceinline__ void store_states(float* s, const ScanParams& p, int64_t unit, int64_t e, int n0,
+                                             const float (&h)[kSlice])
+{
+    float4* at = reinterpret_cast<float4*>(s + (unit * p.E + e) * p.N + n0);
+#pragma unroll
+    for (int k = 0; k < kSlice / 4; ++k) at[k] = make_float4(h[4 * k], h[4 * k + 1], h[4 * k + 2], h[4 * k + 3]);
+}
+
+// A in log2 units: exp(dt A) = exp2(dt A2).
+__device__ __forceinline__ float decay_rate(float a_log) { return -expf(a_log) * kLog2e; }
+
+__device__ __forceinline__ float time_step(const ScanParams& p, float v) { return p.softplus ? softplus_hw(v) : v; }
+
+hipError_t launch_scan_chunk_states(const ScanParams& p, bool bf16, bool marks, hipStream_t stream);
+hipError_t launch_scan_pass(const ScanParams& p, hipStream_t stream);
+
+}  // namespace ssd

@@ -1,0 +1,335 @@
+// The selective scan of the first kind of block: forward and the single-token
+// step.
+//
+//     h_t = exp(dt_t A) h_{t-1} + dt_t x_t B_t,   y_t = h_t . C_t + D x_t,   y_t *= silu(z_t)
+//
+// per channel e with N states n of its own decay A_e,n.  Per (token, channel,
+// state): a product and exp2 for the decay, a product for the input, a multiply-
+// add for the state and one for the output -- bound by vector arithmetic (six
+// issue slots; the matrix cores cannot take a product whose factor differs for
+// every element), not by HBM.
+//
+// The recurrence runs over tokens in registers (ssd_scan.h).  Where the channel
+// tiles alone do not fill the device, the tokens are cut into chunks of L: their
+// states from zero (k_scan_chunk<kStates>), a scan over the chunks
+// (k_scan_pass), then the outputs from each chunk's entering state
+// (k_scan_chunk<kOutput>); the first of the three costs five more slots.
+// Sequences of a packed row replace the state at their first token.
+#include "ssd_internal.h"
+#include "ssd_scan.h"
+
+namespace ssd {
+namespace {
+
+enum Mode { kOutput, kStates, kMarks };
+
+// kOutput: y and final states.  kStates: each chunk's state from zero (from the
+// initial state in the first one) and its sum of dt.  kMarks: the states in front
+// of every tile of kBwdTile tokens, for the gradients.
+// Workgroup: a wavefront per 16 states, at most THREADS / 64 of them (the bound
+// says how many registers a lane may have).
+template <typename T, bool PACKED, Mode MODE, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_scan_chunk(ScanParams p)
+{
+    extern __shared__ float shared[];   // kOutput with several wavefronts: [2][kTok][slices][64]
+    const int slice = THREADS == 64 ? 0 : uniform(threadIdx.x >> 6);
+    const int slices = THREADS == 64 ? 1 : static_cast<int>(p.N / kSlice), lane = threadIdx.x & 63;
+    const ScanWork w = scan_work(p, blockIdx.x);
+    if (MODE == kStates && w.chunk == p.S - 1) return;   // no chunk after it
+    const int n0 = slice * kSlice;
+    const T* x = static_cast<const T*>(p.x) + w.row * p.xb + w.e;
+    const T* dt = static_cast<const T*>(p.dt) + w.row * p.db + w.e;
+    const T* z = MODE == kOutput && p.z ? static_cast<const T*>(p.z) + w.row * p.zb + w.e : nullptr;
+    const T* B = static_cast<const T*>(p.B) + w.row * p.bb + w.g * p.N + n0;
+    const T* C = static_cast<const T*>(p.C) + w.row * p.cb + w.g * p.N + n0;
+    T* y = MODE == kOutput ? static_cast<T*>(p.y) + w.row * p.T * p.E + w.e : nullptr;
+    float A2[kSlice], h[kSlice];
+    load_states(p.A_log, p, 0, w.e, n0, A2);   // (E, N): the layout of one unit
+#pragma unroll
+    for (int n = 0; n < kSlice; ++n) A2[n] = decay_rate(A2[n]);
+    const float bias = p.dt_bias ? p.dt_bias[w.e] : 0.f;
+    const float D = MODE == kOutput && p.D ? p.D[w.e] : 0.f;
+    int64_t unit = scan_unit<PACKED>(p, w.row, w.t0);
+    float* const st = p.states + ((w.row * p.S + w.chunk) * p.N + n0) * p.E + w.e;
+    if (w.chunk == 0) {
+        load_states(p.init, p, unit, w.e, n0, h);
+    } else if (MODE == kStates) {
+#pragma unroll
+        for (int n = 0; n < kSlice; ++n) h[n] = 0.f;
+    } else {
+#pragma unroll
+        for (int n = 0; n < kSlice; ++n) h[n] = st[n * p.E];
+    }
+    float sum = 0.f;
+
+    T xr[kTok], dr[kTok], zr[kTok];   // the present tile's tokens
+    const auto fetch = [&](int64_t t, T (&xv)[kTok], T (&dv)[kTok], T (&zv)[kTok]) {
+#pragma unroll
+        for (int u = 0; u < kTok; ++u) {
+            const int64_t at = t + u < w.t1 ? t + u : w.t1 - 1;
+            xv[u] = x[at * p.xt];
+            dv[u] = dt[at * p.dtt];
+            if (MODE == kOutput && z) zv[u] = z[at * p.zt];
+        }
+    };
+    fetch(w.t0, xr, dr, zr);
+    int buf = 0;
+    for (int64_t t = w.t0; t < w.t1; t += kTok) {
+        if (MODE == kMarks && t % kBwdTile == 0) {
+            float* m = p.marks + ((w.row * ((p.T + kBwdTile - 1) / kBwdTile) + t / kBwdTile) * p.N + n0) * p.E + w.e;
+            if (w.live) {
+#pragma unroll
+                for (int n = 0; n < kSlice; ++n) m[n * p.E] = h[n];
+            }
+        }
+        T xn[kTok], dn[kTok], zn[kTok];
+        fetch(t + kTok < w.t1 ? t + kTok : t, xn, dn, zn);
+        float ys[kTok] = {};
+#pragma unroll
+        for (int u = 0; u < kTok; ++u) {
+            if (t + u >= w.t1) break;
+            if (PACKED && t + u > 0 && scan_starts<PACKED>(p, t + u)) {
+                unit = scan_unit<PACKED>(p, w.row, t + u);
+                load_states(p.init, p, unit, w.e, n0, h);
+            }
+            const float d = time_step(p, widen(dr[u]) + bias), in = d * widen(xr[u]);
+            float b[kSlice], c[kSlice];
+            uniform_row(B + (t + u) * p.bt, b);
+            if (MODE == kOutput) uniform_row(C + (t + u) * p.ct, c);
+            if (MODE == kStates) sum += d;
+            float y0 = 0.f, y1 = 0.f;
+#pragma unroll
+            for (int n = 0; n < kSlice; n += 2) {
+                h[n] = fmaf(__builtin_amdgcn_exp2f(d * A2[n]), h[n], in * b[n]);
+                h[n + 1] = fmaf(__builtin_amdgcn_exp2f(d * A2[n + 1]), h[n + 1], in * b[n + 1]);
+                if (MODE == kOutput) {
+                    y0 = fmaf(h[n], c[n], y0);
+                    y1 = fmaf(h[n + 1], c[n + 1], y1);
+                }
+            }
+            ys[u] = y0 + y1;
+            if (MODE == kOutput && p.fin && w.live && scan_ends<PACKED>(p, t + u))
+                store_states(p.fin, p, unit, w.e, n0, h);
+        }
+        if (MODE == kOutput) {
+            float* part = shared + buf * kTok * slices * 64;
+            if (slices > 1) {
+#pragma unroll
+                for (int u = 0; u < kTok; ++u) part[(u * slices + slice) * 64 + lane] = ys[u];
+                __syncthreads();
+                buf ^= 1;   // (the other half is written next: one barrier a tile is enough)
+            }
+#pragma unroll
+            for (int u = 0; u < kTok; ++u) {
+                if (t + u >= w.t1) break;
+                if (slices > 1) {
+                    if (u % slices != slice) continue;
+                    ys[u] = 0.f;
+                    for (int k = 0; k < slices; ++k) ys[u] += part[(u * slices + k) * 64 + lane];
+                }
+                float v = fmaf(D, widen(xr[u]), ys[u]);
+                if (z) {
+                    const float zv = widen(zr[u]);
+                    v *= zv * sigmoid_hw(zv);
+                }
+                if (w.live) y[(t + u) * p.E] = narrow<T>(v);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kTok; ++u) {
+            xr[u] = xn[u];
+            dr[u] = dn[u];
+            zr[u] = zn[u];
+        }
+    }
+    if (MODE == kStates && w.live) {
+#pragma unroll
+        for (int n = 0; n < kSlice; ++n) st[n * p.E] = h[n];
+        if (slice == 0) p.sums[(w.row * p.S + w.chunk) * p.E + w.e] = sum;
+    }
+}
+
+// The scan over chunks: the states of each chunk (from zero) become the states
+// entering it.  A thread per batch row, state and channel.
+constexpr int kPassBatch = 8;
+
+__global__ __launch_bounds__(256) void k_scan_pass(ScanParams p)
+{
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    if (i >= p.b * p.N * p.E) return;
+    const int64_t e = i % p.E, rn = i / p.E, n = rn % p.N, row = rn / p.N;
+    const float A2 = decay_rate(p.A_log[e * p.N + n]);
+    float* st = p.states + (row * p.S * p.N + n) * p.E + e;
+    const float* sums = p.sums + row * p.S * p.E + e;
+    const int64_t step = p.N * p.E;
+    float h = st[0];
+    for (int64_t c = 1; c < p.S; c += kPassBatch) {
+        float s[kPassBatch], d[kPassBatch];
+#pragma unroll
+        for (int k = 0; k < kPassBatch; ++k) {
+            const int64_t at = c + k < p.S - 1 ? c + k : 0;   // (the last chunk's own state is not needed)
+            s[k] = st[at * step];
+            d[k] = sums[at * p.E];
+        }
+#pragma unroll
+        for (int k = 0; k < kPassBatch; ++k) {
+            if (c + k >= p.S) break;
+            st[(c + k) * step] = h;
+            // the decay in two halves, so that one below 2^-126 still counts
+            const float half = __builtin_amdgcn_exp2f(d[k] * A2 * 0.5f);
+            h = fmaf(h * half, half, s[k]);
+            if (p.seq_idx) {
+                const int64_t t0 = (c + k) * p.L, t1 = t0 + p.L < p.T ? t0 + p.L : p.T;
+                if (p.seq_idx[t0 - 1] != p.seq_idx[t1 - 1]) h = s[k];   // a sequence starts in the chunk
+            }
+        }
+    }
+}
+
+// One token per batch row.  Memory-bound: the state is read and written once.  A
+// thread owns 4 consecutive states (16 bytes), the N / 4 threads of a channel are
+// a power-of-two segment of a wavefront.
+template <typename T>
+__global__ __launch_bounds__(256) void k_scan_step(ScanParams p, int seg, int log2seg)
+{
+    const int64_t i = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) >> log2seg;
+    const int n0 = 4 * (threadIdx.x & (seg - 1));
+    const bool live = i < p.b * p.E && n0 < p.N;
+    float sum = 0.f, xv = 0.f;
+    int64_t row = 0, e = 0;
+    if (live) {
+        row = i / p.E;
+        e = i - row * p.E;
+        const int64_t g = e / (p.E / p.G);
+        const T* B = static_cast<const T*>(p.B) + row * p.bb + g * p.N + n0;
+        const T* C = static_cast<const T*>(p.C) + row * p.cb + g * p.N + n0;
+        float* st = p.fin + i * p.N + n0;
+        const float4 old = *reinterpret_cast<const float4*>(st);
+        const auto a = Pack<float, 4>::load(p.A_log + e * p.N + n0);
+        const auto b = Pack<T, 4>::load(B), c = Pack<T, 4>::load(C);
+        xv = widen(static_cast<const T*>(p.x)[row * p.xb + e]);
+        const float d = time_step(p, widen(static_cast<const T*>(p.dt)[row * p.db + e]) + (p.dt_bias ? p.dt_bias[e] : 0.f));
+        const float in = d * xv, o[4] = {old.x, old.y, old.z, old.w};
+        float h[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            h[k] = fmaf(__builtin_amdgcn_exp2f(d * decay_rate(a[k])), o[k], in * b[k]);
+            sum = fmaf(h[k], c[k], sum);
+        }
+        typedef float f4 __attribute__((ext_vector_type(4)));
+        __builtin_nontemporal_store(f4{h[0], h[1], h[2], h[3]}, reinterpret_cast<f4*>(st));
+    }
+    for (int off = seg >> 1; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
+    if (live && n0 == 0) {
+        if (p.D) sum = fmaf(p.D[e], xv, sum);
+        if (p.z) {
+            const float zv = widen(static_cast<const T*>(p.z)[row * p.zb + e]);
+            sum *= zv * sigmoid_hw(zv);
+        }
+        static_cast<T*>(p.y)[i] = narrow<T>(sum);
+    }
+}
+
+template <typename T, bool PACKED, Mode MODE, int THREADS>
+hipError_t chunk(const ScanParams& p, hipStream_t stream)
+{
+    const int64_t units = p.b * p.S * p.G * scan_tiles(p.E, p.G);
+    const int slices = static_cast<int>(p.N / kSlice);
+    const size_t lds = MODE == kOutput && slices > 1 ? 2 * kTok * slices * 64 * sizeof(float) : 0;
+    if (units > kMaxGrid) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL((k_scan_chunk<T, PACKED, MODE, THREADS>), dim3(static_cast<unsigned>(units)), dim3(64 * slices),
+                       lds, stream, p);
+    return hipGetLastError();
+}
+
+template <typename T, bool PACKED, Mode MODE>
+hipError_t by_states(const ScanParams& p, hipStream_t stream)
+{
+    if (p.N <= kSlice) return chunk<T, PACKED, MODE, 64>(p, stream);
+    if (p.N <= 4 * kSlice) return chunk<T, PACKED, MODE, 256>(p, stream);
+    return chunk<T, PACKED, MODE, 1024>(p, stream);
+}
+
+template <typename T, Mode MODE>
+hipError_t chunks(const ScanParams& p, hipStream_t stream)
+{
+    return p.seq_idx ? by_states<T, true, MODE>(p, stream) : by_states<T, false, MODE>(p, stream);
+}
+
+}  // namespace
+
+hipError_t launch_scan_chunk_states(const ScanParams& p, bool bf16, bool marks, hipStream_t stream)
+{
+    if (marks) return bf16 ? chunks<uint16_t, kMarks>(p, stream) : chunks<float, kMarks>(p, stream);
+    return bf16 ? chunks<uint16_t, kStates>(p, stream) : chunks<float, kStates>(p, stream);
+}
+
+hipError_t launch_scan_pass(const ScanParams& p, hipStream_t stream)
+{
+    const int64_t grid = (p.b * p.N * p.E + 255) / 256;
+    if (grid > kMaxGrid) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL(k_scan_pass, dim3(static_cast<unsigned>(grid)), dim3(256), 0, stream, p);
+    return hipGetLastError();
+}
+
+ScanPlan scan_plan(int64_t b, int64_t T, int64_t E, int64_t N, int64_t G, bool backward)
+{
+    ScanPlan w{};
+    const int64_t tiles = G * scan_tiles(E, G), waves = b * tiles * (N / kSlice);
+    // Chunks: four wavefronts a SIMD (4,096), none shorter than 64 tokens.
+    int64_t S = (4096 + waves - 1) / waves;
+    const int64_t most = T / 64 > 1 ? T / 64 : 1;
+    if (S > most) S = most;
+    const int64_t unit = backward ? kBwdTile : kTok;
+    w.L = ((T + S - 1) / S + unit - 1) / unit * unit;
+    w.S = (T + w.L - 1) / w.L;
+    w.cblocks = scan_tiles(E, G);
+    size_t off = 0;
+    const auto take = [&](int64_t floats) {
+        const size_t at = off;
+        off += (static_cast<size_t>(floats) * sizeof(float) + 255) / 256 * 256;
+        return at;
+    };
+    const int64_t st = b * w.S * N * E;
+    if (w.S > 1) {
+        w.states = take(st);
+        w.sums = take(b * w.S * E);
+    }
+    if (backward) {
+        w.rstates = take(st);
+        w.marks = take(b * ((T + kBwdTile - 1) / kBwdTile) * N * E);
+        w.pA = take(st);
+        w.pD = take(b * w.S * 2 * E);
+        w.pBC = take(w.cblocks * b * T * G * 2 * N);
+    }
+    w.total = off;
+    return w;
+}
+
+hipError_t launch_scan_forward(const ScanParams& p, bool bf16, hipStream_t stream)
+{
+    if (p.S > 1) {
+        hipError_t err = launch_scan_chunk_states(p, bf16, false, stream);
+        if (err == hipSuccess) err = launch_scan_pass(p, stream);
+        if (err != hipSuccess) return err;
+    }
+    return bf16 ? chunks<uint16_t, kOutput>(p, stream) : chunks<float, kOutput>(p, stream);
+}
+
+hipError_t launch_scan_step(const ScanParams& p, bool bf16, hipStream_t stream)
+{
+    int seg = 4, log2seg = 2;
+    while (4 * seg < p.N) {
+        seg <<= 1;
+        ++log2seg;
+    }
+    const int64_t grid = (p.b * p.E * seg + 255) / 256;
+    if (grid > kMaxGrid) return hipErrorInvalidConfiguration;
+    if (bf16)
+        hipLaunchKernelGGL(k_scan_step<uint16_t>, dim3(static_cast<unsigned>(grid)), dim3(256), 0, stream, p, seg, log2seg);
+    else
+        hipLaunchKernelGGL(k_scan_step<float>, dim3(static_cast<unsigned>(grid)), dim3(256), 0, stream, p, seg, log2seg);
+    return hipGetLastError();
+}
+
+}  // namespace ssd

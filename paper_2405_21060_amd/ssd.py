@@ -10,10 +10,15 @@ Names mirror the ABI: :func:`ssd_workspace_bytes`, :func:`ssd_forward`,
 :func:`forward` is the tensor-level convenience wrapper returning
 ``(y, final_states)`` like the paper's ``ssd(X, A, B, C, block_len,
 initial_states)``, :func:`forward_block` the same with the block steps around
-the layer, :func:`decode_step` one recurrent step.
+the layer, :func:`decode_step` one recurrent step.  What stands around the layer
+in a block: :func:`conv_forward`, :func:`conv_backward`, :func:`conv_step` (short
+convolution), :func:`scan_forward`, :func:`scan_backward`, :func:`scan_step`
+(selective scan), :func:`add_norm`, :func:`add_norm_q8`,
+:func:`add_norm_backward` (residual addition and norm).
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Optional, Tuple
@@ -23,6 +28,8 @@ LIB_PATH = os.path.join(HERE, "libssd_hip.so")
 
 SSD_DTYPE_F32 = 0
 SSD_DTYPE_BF16 = 1
+SSD_DTYPE_I8 = 2
+SSD_DTYPE_E4M3 = 3
 SSD_OK = 0
 SSD_ERR_NULL_ARG = -1
 SSD_ERR_BAD_SHAPE = -2
@@ -45,7 +52,11 @@ EXPORTED = ("ssd_workspace_bytes", "ssd_forward", "ssd_forward_timed", "ssd_deco
             "ssd_backward_varlen_workspace_bytes", "ssd_backward_varlen",
             "ssd_forward_varlen_workspace_bytes", "ssd_forward_varlen",
             "ssd_backward_block_workspace_bytes", "ssd_backward_block", "ssd_workspace_status",
-            "ssd_set_tuning", "ssd_forward_noalloc", "ssd_error_string")
+            "ssd_set_tuning", "ssd_forward_noalloc", "ssd_error_string",
+            "ssd_conv_forward", "ssd_conv_backward_workspace_bytes", "ssd_conv_backward", "ssd_conv_step",
+            "ssd_scan_workspace_bytes", "ssd_scan_forward", "ssd_scan_backward_workspace_bytes",
+            "ssd_scan_backward", "ssd_scan_step",
+            "ssd_add_norm", "ssd_add_norm_backward_workspace_bytes", "ssd_add_norm_backward")
 
 
 class SsdProblem(ctypes.Structure):
@@ -72,6 +83,41 @@ class SsdBlockOpts(ctypes.Structure):
         ("norm_weight", ctypes.c_void_p),
         ("norm_group_size", ctypes.c_int64),
         ("norm_eps", ctypes.c_float),
+    ]
+
+
+class SsdConvProblem(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int64),
+        ("seqlen", ctypes.c_int64),
+        ("channels", ctypes.c_int64),
+        ("width", ctypes.c_int64),
+        ("nseq", ctypes.c_int64),
+        ("x_batch_stride", ctypes.c_int64),
+        ("x_token_stride", ctypes.c_int64),
+        ("nparts", ctypes.c_int64),
+        ("parts", ctypes.c_int64 * 3),
+        ("dtype", ctypes.c_int32),
+        ("silu", ctypes.c_int32),
+    ]
+
+
+class SsdScanProblem(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int64) for name in (
+        "batch", "seqlen", "channels", "dstate", "ngroups", "nseq", "x_batch_stride", "x_token_stride",
+        "dt_batch_stride", "dt_token_stride", "z_batch_stride", "z_token_stride", "b_batch_stride",
+        "b_token_stride", "c_batch_stride", "c_token_stride")] + [
+        ("dtype", ctypes.c_int32), ("dt_softplus", ctypes.c_int32)]
+
+
+class SsdNormProblem(ctypes.Structure):
+    _fields_ = [
+        ("rows", ctypes.c_int64),
+        ("channels", ctypes.c_int64),
+        ("dtype", ctypes.c_int32),
+        ("residual_dtype", ctypes.c_int32),
+        ("out_dtype", ctypes.c_int32),
+        ("eps", ctypes.c_float),
     ]
 
 
@@ -148,6 +194,23 @@ def load_library(path: str = LIB_PATH):
     lib.ssd_set_tuning.restype = ctypes.c_int
     lib.ssd_forward_noalloc.argtypes = [ctypes.POINTER(SsdProblem)] + [vp] * 12
     lib.ssd_forward_noalloc.restype = ctypes.c_int
+    cp, sp, np_ = (ctypes.POINTER(t) for t in (SsdConvProblem, SsdScanProblem, SsdNormProblem))
+    size = ctypes.POINTER(ctypes.c_size_t)
+    for name, args in (
+            ("ssd_conv_forward", [cp] + [vp] * 8),
+            ("ssd_conv_backward_workspace_bytes", [cp, size]),
+            ("ssd_conv_backward", [cp] + [vp] * 12 + [ctypes.c_size_t, vp]),
+            ("ssd_conv_step", [cp] + [vp] * 6),
+            ("ssd_scan_workspace_bytes", [sp, size]),
+            ("ssd_scan_forward", [sp] + [vp] * 13 + [ctypes.c_size_t, vp]),
+            ("ssd_scan_backward_workspace_bytes", [sp, size]),
+            ("ssd_scan_backward", [sp] + [vp] * 22 + [ctypes.c_size_t, vp]),
+            ("ssd_scan_step", [sp] + [vp] * 11),
+            ("ssd_add_norm", [np_] + [vp] * 7),
+            ("ssd_add_norm_backward_workspace_bytes", [np_, size]),
+            ("ssd_add_norm_backward", [np_] + [vp] * 8 + [ctypes.c_size_t, vp])):
+        getattr(lib, name).argtypes = args
+        getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib
 
@@ -749,3 +812,412 @@ def forward_varlen(x, dt, A_log, B, C, seq_starts, D=None, chunk_size: int = 256
                             torch.cuda.current_stream(dev).cuda_stream)
     _check_forward(rc, "ssd_forward_varlen", workspace, wsb, need)
     return y, fin
+
+
+# ---- What stands around the layer in a block -------------------------------------------
+
+_NO_GUARD = contextlib.nullcontext()
+
+
+def _device(index: int):
+    """Makes a device current for a call's launches, where it is not already."""
+    import torch
+
+    return _NO_GUARD if torch._C._cuda_getDevice() == index else torch.cuda.device(index)
+
+
+def _act_dtype(x) -> int:
+    import torch
+
+    if x.device.type != "cuda":
+        raise ValueError("tensors must live on a HIP device")
+    if x.dtype == torch.bfloat16:
+        return SSD_DTYPE_BF16
+    if x.dtype == torch.float32:
+        return SSD_DTYPE_F32
+    raise TypeError("x must be float32 or bfloat16")
+
+
+def _check(x, act=(), f32=(), whole=(), strided=()):
+    """Types and devices of a call's tensors, (name, tensor or None, shape)
+    each: ``act`` of x's type, ``f32`` float32, ``whole`` of any type; all of
+    them contiguous but those of ``strided`` (of x's type too), which need a
+    contiguous last dimension."""
+    import torch
+
+    for name, t, shape in tuple(act) + tuple(strided):
+        if t is not None and t.dtype != x.dtype:
+            raise TypeError("%s must have x's dtype" % name)
+    for name, t, shape in f32:
+        if t is not None and t.dtype != torch.float32:
+            raise TypeError("%s must be float32" % name)
+    for name, t, shape in tuple(act) + tuple(f32) + tuple(whole) + tuple(strided):
+        if t is None:
+            continue
+        if t.device != x.device:
+            raise ValueError("%s must be on x's device" % name)
+        if tuple(t.shape) != tuple(shape):
+            raise ValueError("%s must have shape %s, not %s" % (name, tuple(shape), tuple(t.shape)))
+    for name, t, shape in tuple(act) + tuple(f32) + tuple(whole):
+        if t is not None and not t.is_contiguous():
+            raise ValueError("%s must be contiguous" % name)
+    for name, t, shape in strided:
+        if t is not None and t.shape[-1] > 1 and t.stride(-1) != 1:
+            raise ValueError("%s must be contiguous in its last dimension" % name)
+
+
+def _out(out, like_shape, dtype, device, name="out"):
+    import torch
+
+    if out is None:
+        return torch.empty(like_shape, dtype=dtype, device=device)
+    if out.dtype != dtype:
+        raise TypeError("%s must be %s" % (name, dtype))
+    if tuple(out.shape) != tuple(like_shape) or out.device != device or not out.is_contiguous():
+        raise ValueError("%s must be contiguous, of shape %s and on x's device" % (name, tuple(like_shape)))
+    return out
+
+
+def _packed(seq_idx, nseq, T):
+    """The number of sequences of a packed row (read from the device where it is
+    not given), 0 without one."""
+    import torch
+
+    if seq_idx is None:
+        return 0
+    if seq_idx.dtype != torch.int32:
+        raise TypeError("seq_idx must be int32")
+    if tuple(seq_idx.shape) != (1, T):
+        raise ValueError("seq_idx must have shape (1, %d): packed rows use batch 1" % T)
+    n = int(seq_idx[0, -1].item()) + 1 if nseq is None else int(nseq)
+    if not 1 <= n <= T:
+        raise ValueError("a packed row of %d tokens has 1 to %d sequences, not %d" % (T, T, n))
+    return n
+
+
+def _room(workspace, need: int, dev):
+    """``_workspace``, on the call's device."""
+    if workspace is not None and workspace.device != dev:
+        raise ValueError("workspace must be on x's device")
+    return _workspace(workspace, need, dev)
+
+
+def _sized(name, prob):
+    need = ctypes.c_size_t(0)
+    rc = getattr(load_library(), name)(ctypes.byref(prob), ctypes.byref(need))
+    if rc != SSD_OK:
+        raise SsdError(rc, name)
+    return int(need.value)
+
+
+def _done(rc: int, where: str) -> None:
+    if rc != SSD_OK:
+        raise SsdError(rc, where)
+
+
+def _stream(index: int) -> int:
+    import torch
+
+    return torch._C._cuda_getCurrentRawStream(index)
+
+
+def _conv_problem(x, weight, split, silu, nseq, dtype):
+    b, T, C = x.shape
+    split = (C,) if split is None else tuple(int(k) for k in split)
+    if not 1 <= len(split) <= 3 or min(split) < 1 or sum(split) != C:
+        raise ValueError("split must be 1 to 3 positive sizes that add up to %d channels" % C)
+    parts = (ctypes.c_int64 * 3)(*(split + (0,) * (3 - len(split))))
+    return SsdConvProblem(b, T, C, weight.shape[1], nseq, x.stride(0), x.stride(1), len(split), parts, dtype,
+                          int(bool(silu))), split
+
+
+def _pointers(tensors):
+    return (ctypes.c_void_p * len(tensors))(*[t.data_ptr() for t in tensors])
+
+
+def conv_forward(x, weight, bias=None, silu: bool = True, initial_states=None, seq_idx=None,
+                 nseq: Optional[int] = None, split=None, return_final_states: bool = True, out=None):
+    """Short causal depthwise convolution with SiLU (``ssd_conv_forward``);
+    returns ``(y, final_states or None)``.
+
+    x (b,T,C): float32 or bfloat16, the last dimension contiguous (it may be a
+    slice of a wider tensor).  weight (C,W), W in 2..4, and bias (C): float32.
+    initial_states (b|nseq,W-1,C) in x's dtype: the inputs before the first
+    token, oldest first; final_states likewise after the last.  seq_idx (1,T)
+    int32 with nseq sequences: a packed row.  ``split``: sizes of up to three
+    parts of the channels; y is then a tuple of contiguous tensors (b,T,size),
+    as is ``out``.  Launches on torch's current stream of x's device.
+    """
+    dtype = _act_dtype(x)
+    if x.dim() != 3 or weight.dim() != 2:
+        raise ValueError("x must have 3 dimensions and weight 2")
+    b, T, C = x.shape
+    W = weight.shape[1]
+    units = _packed(seq_idx, nseq, T) or b
+    prob, sizes = _conv_problem(x, weight, split, silu, units, dtype)
+    _check(x, act=(("initial_states", initial_states, (units, W - 1, C)),),
+           f32=(("weight", weight, (C, W)), ("bias", bias, (C,))), whole=(("seq_idx", seq_idx, (1, T)),),
+           strided=(("x", x, (b, T, C)),))
+    outs = (None,) * len(sizes) if out is None else (out,) if split is None else tuple(out)
+    if len(outs) != len(sizes):
+        raise ValueError("out must have as many parts as split")
+    ys = tuple(_out(o, (b, T, k), x.dtype, x.device) for o, k in zip(outs, sizes))
+    fin = _out(None, (units, W - 1, C), x.dtype, x.device) if return_final_states else None
+    on = x.get_device()
+    with _device(on):
+        _done(load_library().ssd_conv_forward(ctypes.byref(prob), _ptr(x), _ptr(weight), _ptr(bias),
+                                              _ptr(initial_states), _ptr(seq_idx), _pointers(ys), _ptr(fin),
+                                              _stream(on)), "ssd_conv_forward")
+    return (ys[0] if split is None else ys), fin
+
+
+def conv_backward(x, weight, dy, bias=None, silu: bool = True, initial_states=None, dfinal_states=None, seq_idx=None,
+                  nseq: Optional[int] = None, workspace=None):
+    """Gradients of ``conv_forward`` given dy: a tensor (b,T,C), or a tuple of the
+    parts' tensors where the forward was split.  Returns a dict: dx (b,T,C),
+    dinit (x's dtype), dweight, dbias (float32; dbias None without a bias)."""
+    import torch
+
+    dtype = _act_dtype(x)
+    if x.dim() != 3 or weight.dim() != 2:
+        raise ValueError("x must have 3 dimensions and weight 2")
+    b, T, C = x.shape
+    W = weight.shape[1]
+    units = _packed(seq_idx, nseq, T) or b
+    dys = (dy,) if isinstance(dy, torch.Tensor) else tuple(dy)
+    prob, sizes = _conv_problem(x, weight, [t.shape[-1] for t in dys], silu, units, dtype)
+    state = (units, W - 1, C)
+    _check(x, act=[("dy", t, (b, T, k)) for t, k in zip(dys, sizes)] + [
+        ("initial_states", initial_states, state), ("dfinal_states", dfinal_states, state)],
+        f32=(("weight", weight, (C, W)), ("bias", bias, (C,))), whole=(("seq_idx", seq_idx, (1, T)),),
+        strided=(("x", x, (b, T, C)),))
+    need = _sized("ssd_conv_backward_workspace_bytes", prob)
+    workspace = _room(workspace, need, x.device)
+    g = {"dx": torch.empty((b, T, C), dtype=x.dtype, device=x.device), "dweight": torch.empty_like(weight),
+         "dbias": torch.empty_like(bias) if bias is not None else None,
+         "dinit": torch.empty(state, dtype=x.dtype, device=x.device)}
+    on = x.get_device()
+    with _device(on):
+        _done(load_library().ssd_conv_backward(
+            ctypes.byref(prob), _ptr(x), _ptr(weight), _ptr(bias), _ptr(initial_states), _ptr(seq_idx), _pointers(dys),
+            _ptr(dfinal_states), _ptr(g["dx"]), _ptr(g["dweight"]), _ptr(g["dbias"]), _ptr(g["dinit"]),
+            _ptr(workspace), need, _stream(on)), "ssd_conv_backward")
+    return g
+
+
+def conv_step(x, weight, state, bias=None, silu: bool = True, out=None):
+    """One token of ``conv_forward`` per row: x (b,C) (rows may be strided), state
+    (b,W-1,C) in x's dtype, moved on in place; returns y (b,C)."""
+    dtype = _act_dtype(x)
+    if x.dim() != 2 or weight.dim() != 2:
+        raise ValueError("x and weight must have 2 dimensions")
+    b, C = x.shape
+    W = weight.shape[1]
+    _check(x, act=(("state", state, (b, W - 1, C)),), f32=(("weight", weight, (C, W)), ("bias", bias, (C,))),
+           strided=(("x", x, (b, C)),))
+    y = _out(out, (b, C), x.dtype, x.device)
+    prob = SsdConvProblem(b, 1, C, W, 0, x.stride(0), 0, 1, (ctypes.c_int64 * 3)(C, 0, 0), dtype, int(bool(silu)))
+    on = x.get_device()
+    with _device(on):
+        _done(load_library().ssd_conv_step(ctypes.byref(prob), _ptr(x), _ptr(weight), _ptr(bias), _ptr(state), _ptr(y),
+                                           _stream(on)), "ssd_conv_step")
+    return y
+
+
+def _scan_problem(x, dt, B, C, z, softplus, nseq, dtype):
+    def strides(t):
+        return (t.stride(0), t.stride(1)) if t is not None else (0, 0)
+
+    b, T, E = x.shape
+    return SsdScanProblem(b, T, E, B.shape[3], B.shape[2], nseq, *strides(x), *strides(dt), *strides(z), *strides(B),
+                          *strides(C), dtype, int(bool(softplus)))
+
+
+def _scan_checked(x, dt, A_log, B, C, D, z, dt_bias, initial_states, seq_idx, nseq, softplus, more_act=(), more_f32=()):
+    """The checks that the scan's forward and gradients share; returns the problem
+    and the number of sequences."""
+    dtype = _act_dtype(x)
+    if x.dim() != 3 or B.dim() != 4:
+        raise ValueError("x must have 3 dimensions and B and C 4")
+    b, T, E = x.shape
+    G, N = B.shape[2:]
+    units = _packed(seq_idx, nseq, T) or b
+    for name, t in (("B", B), ("C", C)):
+        if t.dim() == 4 and G > 1 and t.stride(2) != N:
+            raise ValueError("%s's groups must be contiguous" % name)
+    state = (units, E, N)
+    _check(x, act=more_act, f32=[("A_log", A_log, (E, N)), ("D", D, (E,)), ("dt_bias", dt_bias, (E,)),
+                                 ("initial_states", initial_states, state)] + [(n, t, state) for n, t in more_f32],
+           whole=(("seq_idx", seq_idx, (1, T)),),
+           strided=(("x", x, (b, T, E)), ("dt", dt, (b, T, E)), ("z", z, (b, T, E)), ("B", B, (b, T, G, N)),
+                    ("C", C, (b, T, G, N))))
+    return _scan_problem(x, dt, B, C, z, softplus, units, dtype), units
+
+
+def scan_forward(x, dt, A_log, B, C, D=None, z=None, dt_bias=None, dt_softplus: bool = True, initial_states=None,
+                 seq_idx=None, nseq: Optional[int] = None, return_final_states: bool = True, workspace=None, out=None,
+                 final_out=None) -> Tuple[object, object]:
+    """Selective scan (``ssd_scan_forward``): a decay exp(dt A) of its own for every
+    channel and state, A = -exp(A_log); returns ``(y, final_states or None)``.
+
+    x, dt, z (b,T,E), B, C (b,T,G,N): float32 or bfloat16, the same dtype, the last
+    dimension (of B and C the last two) contiguous; N a multiple of 16 up to 256.
+    A_log (E,N), D, dt_bias (E): float32.  dt is raw: softplus(dt + dt_bias), or
+    dt + dt_bias without ``dt_softplus``.  The output is gated by SiLU(z) when z is
+    given.  initial_states (b|nseq,E,N) float32.  seq_idx (1,T) int32 with nseq
+    sequences.  Launches on torch's current stream of x's device.
+    """
+    import torch
+
+    prob, units = _scan_checked(x, dt, A_log, B, C, D, z, dt_bias, initial_states, seq_idx, nseq, dt_softplus)
+    b, T, E = x.shape
+    need = _sized("ssd_scan_workspace_bytes", prob)
+    workspace = _room(workspace, need, x.device)
+    y = _out(out, (b, T, E), x.dtype, x.device)
+    fin = None
+    if return_final_states:
+        fin = _out(final_out, (units, E, B.shape[3]), torch.float32, x.device, "final_out")
+    on = x.get_device()
+    with _device(on):
+        _done(load_library().ssd_scan_forward(
+            ctypes.byref(prob), _ptr(x), _ptr(dt), _ptr(A_log), _ptr(B), _ptr(C), _ptr(D), _ptr(z), _ptr(dt_bias),
+            _ptr(initial_states), _ptr(seq_idx), _ptr(y), _ptr(fin), _ptr(workspace), need, _stream(on)),
+            "ssd_scan_forward")
+    return y, fin
+
+
+def scan_backward(x, dt, A_log, B, C, dy, D=None, z=None, dt_bias=None, dt_softplus: bool = True, initial_states=None,
+                  dfinal_states=None, seq_idx=None, nseq: Optional[int] = None, workspace=None):
+    """Gradients of ``scan_forward`` given dy (and optionally the gradient of the
+    final states).  Returns a dict: dx, ddt (of the raw dt), dB, dC, dz (x's dtype;
+    dz None without z), dA_log, dD, ddt_bias, dinit (float32; dD and ddt_bias None
+    where the input is absent)."""
+    import torch
+
+    prob, units = _scan_checked(x, dt, A_log, B, C, D, z, dt_bias, initial_states, seq_idx, nseq, dt_softplus,
+                                more_act=(("dy", dy, tuple(x.shape)),), more_f32=(("dfinal_states", dfinal_states),))
+    need = _sized("ssd_scan_backward_workspace_bytes", prob)
+    workspace = _room(workspace, need, x.device)
+
+    def new(t, kind=None):
+        return torch.empty(t.shape, dtype=kind or t.dtype, device=t.device) if t is not None else None
+
+    g = {"dx": new(x), "ddt": new(x), "dB": new(B), "dC": new(C), "dz": new(z), "dA_log": new(A_log), "dD": new(D),
+         "ddt_bias": new(dt_bias),
+         "dinit": torch.empty((units, x.shape[2], B.shape[3]), dtype=torch.float32, device=x.device)}
+    on = x.get_device()
+    with _device(on):
+        _done(load_library().ssd_scan_backward(
+            ctypes.byref(prob), _ptr(x), _ptr(dt), _ptr(A_log), _ptr(B), _ptr(C), _ptr(D), _ptr(z), _ptr(dt_bias),
+            _ptr(initial_states), _ptr(seq_idx), _ptr(dy), _ptr(dfinal_states), _ptr(g["dx"]), _ptr(g["ddt"]),
+            _ptr(g["dA_log"]), _ptr(g["dB"]), _ptr(g["dC"]), _ptr(g["dD"]), _ptr(g["dz"]), _ptr(g["ddt_bias"]),
+            _ptr(g["dinit"]), _ptr(workspace), need, _stream(on)), "ssd_scan_backward")
+    return g
+
+
+def scan_step(x, dt, A_log, B, C, state, D=None, z=None, dt_bias=None, dt_softplus: bool = True, out=None):
+    """One token of ``scan_forward`` per row: x, dt, z (b,E), B, C (b,G,N) (rows may be
+    strided), state (b,E,N) float32, updated in place; returns y (b,E)."""
+    dtype = _act_dtype(x)
+    if x.dim() != 2 or B.dim() != 3:
+        raise ValueError("x must have 2 dimensions and B and C 3")
+    b, E = x.shape
+    G, N = B.shape[1:]
+    for name, t in (("B", B), ("C", C)):
+        if t.dim() == 3 and G > 1 and t.stride(1) != N:
+            raise ValueError("%s's groups must be contiguous" % name)
+    _check(x, f32=(("A_log", A_log, (E, N)), ("D", D, (E,)), ("dt_bias", dt_bias, (E,)), ("state", state, (b, E, N))),
+           strided=(("x", x, (b, E)), ("dt", dt, (b, E)), ("z", z, (b, E)), ("B", B, (b, G, N)), ("C", C, (b, G, N))))
+    y = _out(out, (b, E), x.dtype, x.device)
+    prob = SsdScanProblem(b, 1, E, N, G, 0, x.stride(0), 0, dt.stride(0), 0, z.stride(0) if z is not None else 0, 0,
+                          B.stride(0), 0, C.stride(0), 0, dtype, int(bool(dt_softplus)))
+    on = x.get_device()
+    with _device(on):
+        _done(load_library().ssd_scan_step(ctypes.byref(prob), _ptr(x), _ptr(dt), _ptr(A_log), _ptr(B), _ptr(C),
+                                           _ptr(D), _ptr(z), _ptr(dt_bias), _ptr(state), _ptr(y), _stream(on)),
+              "ssd_scan_step")
+    return y
+
+
+def _norm_checked(x, weight, residual, residual_dtype, act=(), whole=()):
+    """Rows, channels and the residual's dtype of a norm's call."""
+    import torch
+
+    dtype = _act_dtype(x)
+    if x.dim() < 1:
+        raise ValueError("x must have at least one dimension")
+    C = x.shape[-1]
+    kind = residual.dtype if residual is not None else residual_dtype or x.dtype
+    if residual is not None and residual_dtype is not None and residual.dtype != residual_dtype:
+        raise TypeError("residual must have residual_dtype")
+    if kind != torch.float32 and kind != x.dtype:
+        raise TypeError("residual must be float32 or have x's dtype")
+    _check(x, act=[("x", x, x.shape)] + [(n, t, x.shape) for n, t in act], f32=(("weight", weight, (C,)),),
+           whole=[("residual", residual, x.shape)] + [(n, t, x.shape) for n, t in whole])
+    return dtype, SSD_DTYPE_F32 if kind == torch.float32 else SSD_DTYPE_BF16, kind, x.numel() // C if C else 0, C
+
+
+def _add_norm(x, weight, residual, eps, residual_dtype, out_type, out_dtype, scaled):
+    import torch
+
+    dtype, res, kind, rows, C = _norm_checked(x, weight, residual, residual_dtype)
+    # without a residual and in x's own dtype, r is x
+    keep = residual is not None or kind != x.dtype
+    r = torch.empty(x.shape, dtype=kind, device=x.device) if keep else x
+    y = torch.empty(x.shape, dtype=out_type or x.dtype, device=x.device)
+    scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if scaled else None
+    prob = SsdNormProblem(rows, C, dtype, res, dtype if out_dtype is None else out_dtype, float(eps))
+    on = x.get_device()
+    with _device(on):
+        _done(load_library().ssd_add_norm(ctypes.byref(prob), _ptr(x), _ptr(residual), _ptr(weight), _ptr(y),
+                                          _ptr(scale), _ptr(r) if keep else None, _stream(on)), "ssd_add_norm")
+    return y, scale, r
+
+
+def add_norm(x, weight=None, residual=None, eps: float = 1e-5, residual_dtype=None):
+    """Residual addition and RMS norm (``ssd_add_norm``): returns ``(y, r)``, r = x +
+    residual in the residual's dtype (x's, or float32; ``residual_dtype`` where there
+    is no residual yet) and y = r / sqrt(mean(r^2) + eps) * weight in x's dtype, over
+    the last dimension.  Without a residual and in x's dtype r is x itself.  x and
+    residual are contiguous, weight (C,) float32."""
+    y, _, r = _add_norm(x, weight, residual, eps, residual_dtype, None, None, False)
+    return y, r
+
+
+def add_norm_q8(x, weight=None, residual=None, eps: float = 1e-5, residual_dtype=None, dtype=None):
+    """``add_norm`` with an 8-bit output for an 8-bit projection: returns ``(q, scale,
+    r)``, q in ``dtype`` (torch.int8 or torch.float8_e4m3fn, the default) and scale
+    float32 per row, y ~ q * scale (the row's largest value is at the top of the
+    type's range).  A row with a NaN or an infinity has scale NaN."""
+    import torch
+
+    kinds = {torch.int8: SSD_DTYPE_I8, torch.float8_e4m3fn: SSD_DTYPE_E4M3}
+    dtype = torch.float8_e4m3fn if dtype is None else dtype
+    if dtype not in kinds:
+        raise TypeError("dtype must be torch.int8 or torch.float8_e4m3fn")
+    return _add_norm(x, weight, residual, eps, residual_dtype, dtype, kinds[dtype], True)
+
+
+def add_norm_backward(dy, residual, weight=None, dresidual=None, eps: float = 1e-5, workspace=None):
+    """Gradients of ``add_norm``, given its r (``residual``), dy and the gradient of r
+    (``dresidual``, in r's dtype).  Returns a dict: dx (dy's dtype), dresidual (r's
+    dtype; the same tensor as dx where the types are the same), dweight (float32, None
+    without a weight)."""
+    import torch
+
+    dtype, res, kind, rows, C = _norm_checked(dy, weight, residual, None, whole=(("dresidual", dresidual),))
+    if dresidual is not None and dresidual.dtype != kind:
+        raise TypeError("dresidual must have residual's dtype")
+    prob = SsdNormProblem(rows, C, dtype, res, dtype, float(eps))
+    need = _sized("ssd_add_norm_backward_workspace_bytes", prob) if weight is not None else 0
+    workspace = _room(workspace, need, dy.device) if weight is not None else None
+    dx = torch.empty_like(dy)
+    dr = dx if kind == dy.dtype else torch.empty(dy.shape, dtype=kind, device=dy.device)
+    g = {"dx": dx, "dresidual": dr, "dweight": torch.empty_like(weight) if weight is not None else None}
+    on = dy.get_device()
+    with _device(on):
+        _done(load_library().ssd_add_norm_backward(
+            ctypes.byref(prob), _ptr(dy), _ptr(residual), _ptr(weight), _ptr(dresidual), _ptr(dx),
+            None if dr is dx else _ptr(dr), _ptr(g["dweight"]), _ptr(workspace), need, _stream(on)),
+            "ssd_add_norm_backward")
+    return g
