@@ -19,7 +19,9 @@ constexpr int kBwdTile = 16;   // tokens per tile of the gradients
 // A wavefront's place: channel tile (64 channels of one group), chunk, batch row.
 struct ScanWork {
     int64_t row, chunk, t0, t1;
-    int64_t g, e;      // group, the lane's channel (a lane past its group's end: the last one)
+    int64_t g, e0;     // group, first channel
+    unsigned lane;     // the lane's channel from there (a lane past its group's end: the last one)
+    int64_t e;         // the same, from 0
     int64_t tile;      // channel tile within the group
     bool live;
 };
@@ -37,9 +39,12 @@ __device__ __forceinline__ ScanWork scan_work(const ScanParams& p, int64_t unit)
     w.t1 = w.t0 + p.L < p.T ? w.t0 + p.L : p.T;
     w.g = tile / per;
     w.tile = tile - w.g * per;
-    const int64_t e = w.tile * 64 + (threadIdx.x & 63);
-    w.live = e < eg;
-    w.e = w.g * eg + (w.live ? e : eg - 1);
+    w.e0 = w.g * eg + w.tile * 64;
+    const int64_t left = eg - w.tile * 64;
+    const unsigned lane = threadIdx.x & 63;
+    w.live = lane < left;
+    w.lane = w.live ? lane : static_cast<unsigned>(left - 1);
+    w.e = w.e0 + w.lane;
     return w;
 }
 
@@ -67,22 +72,57 @@ __device__ __forceinline__ bool scan_ends(const ScanParams& p, int64_t t)
     return scalar_load(p.seq_idx + t) != scalar_load(p.seq_idx + t + 1);
 }
 
+// Keeps a running scalar as it is: the compiler would otherwise make it anew for
+// every token, by 64-bit products of the token and the stride.
+template <typename P>
+__device__ __forceinline__ void running(P& p) { asm volatile("" : "+s"(p)); }
+
+// A tensor's row of a token, walked from token to token: a uniform pointer and the
+// lane's offset.
+template <typename T>
+struct Rows {
+    typedef __attribute__((address_space(1))) T* pointer;
+    pointer p;
+    int step;   // elements to the next token's row
+
+    __device__ __forceinline__ Rows(const void* base, int64_t first, int64_t stride)
+        : p((pointer)(reinterpret_cast<uintptr_t>(base) + first * sizeof(T))), step(static_cast<int>(stride)) {}
+    __device__ __forceinline__ T get(unsigned lane) const { return p[lane]; }
+    __device__ __forceinline__ void put(unsigned lane, T v) const { p[lane] = v; }
+    __device__ __forceinline__ void move(bool on = true)
+    {
+        p += on ? step : 0;
+        running(p);
+    }
+    __device__ __forceinline__ void back(bool on = true)
+    {
+        p -= on ? step : 0;
+        running(p);
+    }
+    // K uniform values (4-byte aligned), through the scalar cache.
+    template <int K>
+    __device__ __forceinline__ void uniform(float (&v)[K]) const
+    {
+        constexpr int D = K * sizeof(T) / 4;
+        typedef uint32_t words __attribute__((ext_vector_type(D), aligned(4)));
+        const words w = *reinterpret_cast<const __attribute__((address_space(4))) words*>((uintptr_t)p);
+#pragma unroll
+        for (int i = 0; i < D; ++i) {
+            if constexpr (sizeof(T) == 4) {
+                v[i] = __uint_as_float(w[i]);
+            } else {
+                v[2 * i] = __uint_as_float(w[i] << 16);
+                v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+            }
+        }
+    }
+};
+
 // K uniform values at a 4-byte aligned address, through the scalar cache.
 template <typename T, int K>
 __device__ __forceinline__ void uniform_row(const T* at, float (&v)[K])
 {
-    constexpr int D = K * sizeof(T) / 4;
-    typedef uint32_t words __attribute__((ext_vector_type(D), aligned(4)));
-    const words w = *reinterpret_cast<const __attribute__((address_space(4))) words*>(reinterpret_cast<uintptr_t>(at));
-#pragma unroll
-    for (int i = 0; i < D; ++i) {
-        if constexpr (sizeof(T) == 4) {
-            v[i] = __uint_as_float(w[i]);
-        } else {
-            v[2 * i] = __uint_as_float(w[i] << 16);
-            v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-        }
-    }
+    Rows<T>(at, 0, 0).uniform(v);
 }
 
 // A lane's 16 states of a unit, in the caller's layout (units, E, N).

@@ -28,27 +28,35 @@ enum Mode { kOutput, kStates, kMarks };
 // of every tile of kBwdTile tokens, for the gradients.
 // Workgroup: a wavefront per 16 states, at most THREADS / 64 of them (the bound
 // says how many registers a lane may have).
+//
+// A tile is kTok tokens, held in registers; each token's place is loaded anew for
+// the tile after as soon as it has been used.  With several wavefronts their shares
+// of y meet in shared memory, and wavefront k finishes every token u = k, k +
+// slices, ..
 template <typename T, bool PACKED, Mode MODE, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_scan_chunk(ScanParams p)
 {
     extern __shared__ float shared[];   // kOutput with several wavefronts: [2][kTok][slices][64]
-    const int slice = THREADS == 64 ? 0 : uniform(threadIdx.x >> 6);
-    const int slices = THREADS == 64 ? 1 : static_cast<int>(p.N / kSlice), lane = threadIdx.x & 63;
+    constexpr bool kOne = THREADS == 64, kOut = MODE == kOutput;
+    const int slice = kOne ? 0 : uniform(threadIdx.x >> 6);
+    const int slices = kOne ? 1 : static_cast<int>(p.N / kSlice);
+    const unsigned col = threadIdx.x & 63;
     const ScanWork w = scan_work(p, blockIdx.x);
     if (MODE == kStates && w.chunk == p.S - 1) return;   // no chunk after it
     const int n0 = slice * kSlice;
-    const T* x = static_cast<const T*>(p.x) + w.row * p.xb + w.e;
-    const T* dt = static_cast<const T*>(p.dt) + w.row * p.db + w.e;
-    const T* z = MODE == kOutput && p.z ? static_cast<const T*>(p.z) + w.row * p.zb + w.e : nullptr;
-    const T* B = static_cast<const T*>(p.B) + w.row * p.bb + w.g * p.N + n0;
-    const T* C = static_cast<const T*>(p.C) + w.row * p.cb + w.g * p.N + n0;
-    T* y = MODE == kOutput ? static_cast<T*>(p.y) + w.row * p.T * p.E + w.e : nullptr;
+    const bool gate = kOut && p.z;
+    Rows<const T> x(p.x, w.row * p.xb + w.t0 * p.xt + w.e0, p.xt);
+    Rows<const T> dt(p.dt, w.row * p.db + w.t0 * p.dtt + w.e0, p.dtt);
+    Rows<const T> z(gate ? p.z : p.x, gate ? w.row * p.zb + w.t0 * p.zt + w.e0 : 0, gate ? p.zt : 0);
+    Rows<const T> B(p.B, w.row * p.bb + w.t0 * p.bt + w.g * p.N + n0, p.bt);
+    Rows<const T> C(p.C, w.row * p.cb + w.t0 * p.ct + w.g * p.N + n0, p.ct);
+    Rows<T> y(p.y, (w.row * p.T + w.t0) * p.E + w.e0, p.E);
     float A2[kSlice], h[kSlice];
     load_states(p.A_log, p, 0, w.e, n0, A2);   // (E, N): the layout of one unit
 #pragma unroll
     for (int n = 0; n < kSlice; ++n) A2[n] = decay_rate(A2[n]);
     const float bias = p.dt_bias ? p.dt_bias[w.e] : 0.f;
-    const float D = MODE == kOutput && p.D ? p.D[w.e] : 0.f;
+    const float D = kOut && p.D ? p.D[w.e] : 0.f;
     int64_t unit = scan_unit<PACKED>(p, w.row, w.t0);
     float* const st = p.states + ((w.row * p.S + w.chunk) * p.N + n0) * p.E + w.e;
     if (w.chunk == 0) {
@@ -62,86 +70,96 @@ __global__ __launch_bounds__(THREADS) void k_scan_chunk(ScanParams p)
     }
     float sum = 0.f;
 
-    T xr[kTok], dr[kTok], zr[kTok];   // the present tile's tokens
-    const auto fetch = [&](int64_t t, T (&xv)[kTok], T (&dv)[kTok], T (&zv)[kTok]) {
-#pragma unroll
-        for (int u = 0; u < kTok; ++u) {
-            const int64_t at = t + u < w.t1 ? t + u : w.t1 - 1;
-            xv[u] = x[at * p.xt];
-            dv[u] = dt[at * p.dtt];
-            if (MODE == kOutput && z) zv[u] = z[at * p.zt];
-        }
+    const int count = static_cast<int>(w.t1 - w.t0);
+    int ahead = 0;   // the token that the pointers of x, dt and z are at
+    T xr[kTok], dr[kTok], zr[kTok];
+    const auto fetch = [&](int u) {
+        xr[u] = x.get(w.lane);
+        dr[u] = dt.get(w.lane);
+        if (gate) zr[u] = z.get(w.lane);
+        const bool more = ahead + 1 < count;   // (past the end: the last token again)
+        x.move(more);
+        dt.move(more);
+        if (gate) z.move(more);
+        ++ahead;
     };
-    fetch(w.t0, xr, dr, zr);
-    int buf = 0;
-    for (int64_t t = w.t0; t < w.t1; t += kTok) {
+#pragma unroll
+    for (int u = 0; u < kTok; ++u) fetch(u);
+    float* part = shared;
+    for (int t = 0; t < count; t += kTok) {
         if (MODE == kMarks && t % kBwdTile == 0) {
-            float* m = p.marks + ((w.row * ((p.T + kBwdTile - 1) / kBwdTile) + t / kBwdTile) * p.N + n0) * p.E + w.e;
+            const int64_t tile = (w.t0 + t) / kBwdTile, tiles = (p.T + kBwdTile - 1) / kBwdTile;
+            float* m = p.marks + ((w.row * tiles + tile) * p.N + n0) * p.E + w.e;
             if (w.live) {
 #pragma unroll
                 for (int n = 0; n < kSlice; ++n) m[n * p.E] = h[n];
             }
         }
-        T xn[kTok], dn[kTok], zn[kTok];
-        fetch(t + kTok < w.t1 ? t + kTok : t, xn, dn, zn);
-        float ys[kTok] = {};
+        float xs[kTok], zs[kTok];   // several wavefronts: x and z for the end of the tile
 #pragma unroll
         for (int u = 0; u < kTok; ++u) {
-            if (t + u >= w.t1) break;
-            if (PACKED && t + u > 0 && scan_starts<PACKED>(p, t + u)) {
-                unit = scan_unit<PACKED>(p, w.row, t + u);
-                load_states(p.init, p, unit, w.e, n0, h);
+            if (t + u >= count) break;
+            if (PACKED) {
+                if (w.t0 + t + u > 0 && scan_starts<PACKED>(p, w.t0 + t + u)) {
+                    unit = scan_unit<PACKED>(p, w.row, w.t0 + t + u);
+                    load_states(p.init, p, unit, w.e, n0, h);
+                }
             }
-            const float d = time_step(p, widen(dr[u]) + bias), in = d * widen(xr[u]);
+            const float xv = widen(xr[u]), zv = gate ? widen(zr[u]) : 0.f;
+            const float d = time_step(p, widen(dr[u]) + bias), in = d * xv;
+            fetch(u);
             float b[kSlice], c[kSlice];
-            uniform_row(B + (t + u) * p.bt, b);
-            if (MODE == kOutput) uniform_row(C + (t + u) * p.ct, c);
+            B.uniform(b);
+            B.move();
+            if (kOut) {
+                C.uniform(c);
+                C.move();
+            }
             if (MODE == kStates) sum += d;
             float y0 = 0.f, y1 = 0.f;
 #pragma unroll
             for (int n = 0; n < kSlice; n += 2) {
                 h[n] = fmaf(__builtin_amdgcn_exp2f(d * A2[n]), h[n], in * b[n]);
                 h[n + 1] = fmaf(__builtin_amdgcn_exp2f(d * A2[n + 1]), h[n + 1], in * b[n + 1]);
-                if (MODE == kOutput) {
+                if (kOut) {
                     y0 = fmaf(h[n], c[n], y0);
                     y1 = fmaf(h[n + 1], c[n + 1], y1);
                 }
             }
-            ys[u] = y0 + y1;
-            if (MODE == kOutput && p.fin && w.live && scan_ends<PACKED>(p, t + u))
-                store_states(p.fin, p, unit, w.e, n0, h);
-        }
-        if (MODE == kOutput) {
-            float* part = shared + buf * kTok * slices * 64;
-            if (slices > 1) {
-#pragma unroll
-                for (int u = 0; u < kTok; ++u) part[(u * slices + slice) * 64 + lane] = ys[u];
-                __syncthreads();
-                buf ^= 1;   // (the other half is written next: one barrier a tile is enough)
+            if (kOut) {
+                if (PACKED && p.fin && w.live && scan_ends<PACKED>(p, w.t0 + t + u))
+                    store_states(p.fin, p, unit, w.e, n0, h);
+                if (kOne) {
+                    float v = fmaf(D, xv, y0 + y1);
+                    if (gate) v *= zv * sigmoid_hw(zv);
+                    if (w.live) y.put(w.lane, narrow<T>(v));
+                    y.move();
+                } else {
+                    part[(u * slices + slice) * 64 + col] = y0 + y1;
+                    xs[u] = xv;
+                    zs[u] = zv;
+                }
             }
+        }
+        if (kOut && !kOne) {
+            __syncthreads();
 #pragma unroll
             for (int u = 0; u < kTok; ++u) {
-                if (t + u >= w.t1) break;
-                if (slices > 1) {
-                    if (u % slices != slice) continue;
-                    ys[u] = 0.f;
-                    for (int k = 0; k < slices; ++k) ys[u] += part[(u * slices + k) * 64 + lane];
+                if (t + u >= count) break;
+                if (u % slices == slice) {
+                    float v = 0.f;
+                    for (int k = 0; k < slices; ++k) v += part[(u * slices + k) * 64 + col];
+                    v = fmaf(D, xs[u], v);
+                    if (gate) v *= zs[u] * sigmoid_hw(zs[u]);
+                    if (w.live) y.put(w.lane, narrow<T>(v));
                 }
-                float v = fmaf(D, widen(xr[u]), ys[u]);
-                if (z) {
-                    const float zv = widen(zr[u]);
-                    v *= zv * sigmoid_hw(zv);
-                }
-                if (w.live) y[(t + u) * p.E] = narrow<T>(v);
+                y.move();
             }
-        }
-#pragma unroll
-        for (int u = 0; u < kTok; ++u) {
-            xr[u] = xn[u];
-            dr[u] = dn[u];
-            zr[u] = zn[u];
+            // (the other half is written next, so one barrier a tile is enough)
+            part = part == shared ? shared + kTok * slices * 64 : shared;
         }
     }
+    if (kOut && !PACKED && p.fin && w.live && w.t1 == p.T) store_states(p.fin, p, unit, w.e, n0, h);
     if (MODE == kStates && w.live) {
 #pragma unroll
         for (int n = 0; n < kSlice; ++n) st[n * p.E] = h[n];
