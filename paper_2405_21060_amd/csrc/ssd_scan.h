@@ -99,22 +99,27 @@ struct Rows {
         p -= on ? step : 0;
         running(p);
     }
-    // K uniform values (4-byte aligned), through the scalar cache.
-    template <int K>
-    __device__ __forceinline__ void uniform(float (&v)[K]) const
+};
+
+// K uniform values (4-byte aligned) of a row, through the scalar cache: the words
+// as they were read, and what they hold.
+template <typename T, int K>
+struct Uniform {
+    static constexpr int D = K * sizeof(T) / 4;
+    typedef uint32_t words __attribute__((ext_vector_type(D)));
+    typedef uint32_t words_in_memory __attribute__((ext_vector_type(D), aligned(4)));
+    words w;
+
+    __device__ __forceinline__ void load(const Rows<const T>& r)
     {
-        constexpr int D = K * sizeof(T) / 4;
-        typedef uint32_t words __attribute__((ext_vector_type(D), aligned(4)));
-        const words w = *reinterpret_cast<const __attribute__((address_space(4))) words*>((uintptr_t)p);
-#pragma unroll
-        for (int i = 0; i < D; ++i) {
-            if constexpr (sizeof(T) == 4) {
-                v[i] = __uint_as_float(w[i]);
-            } else {
-                v[2 * i] = __uint_as_float(w[i] << 16);
-                v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-            }
-        }
+        w = *reinterpret_cast<const __attribute__((address_space(4))) words_in_memory*>((uintptr_t)r.p);
+    }
+    // Waits for the words here, so that loads issued after are not waited for.
+    __device__ __forceinline__ void arrive() { asm volatile("" : "+s"(w)); }
+    __device__ __forceinline__ float operator[](int i) const
+    {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+        return __uint_as_float(i % 2 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
     }
 };
 
@@ -122,7 +127,10 @@ struct Rows {
 template <typename T, int K>
 __device__ __forceinline__ void uniform_row(const T* at, float (&v)[K])
 {
-    Rows<T>(at, 0, 0).uniform(v);
+    Uniform<T, K> u;
+    u.load(Rows<const T>(at, 0, 0));
+#pragma unroll
+    for (int i = 0; i < K; ++i) v[i] = u[i];
 }
 
 // A lane's 16 states of a unit, in the caller's layout (units, E, N).
@@ -154,7 +162,7 @@ __device__ __forceinline__ void store_states(float* s, const ScanParams& p, int6
 }
 
 // A in log2 units: exp(dt A) = exp2(dt A2).
-__device__ __forceinline__ float decay_rate(float a_log) { return -expf(a_log) * kLog2e; }
+__device__ __forceinline__ float decay_rate(float a_log) { return exp_neg(-a_log) * -kLog2e; }
 
 __device__ __forceinline__ float time_step(const ScanParams& p, float v) { return p.softplus ? softplus_hw(v) : v; }
 

@@ -29,8 +29,8 @@ enum Mode { kOutput, kStates, kMarks };
 // Workgroup: a wavefront per 16 states, at most THREADS / 64 of them (the bound
 // says how many registers a lane may have).
 //
-// A tile is kTok tokens, held in registers; each token's place is loaded anew for
-// the tile after as soon as it has been used.  With several wavefronts their shares
+// A tile is kTok tokens; the next one's are loaded, and its B and C a token ahead,
+// before they are needed.  With several wavefronts their shares
 // of y meet in shared memory, and wavefront k finishes every token u = k, k +
 // slices, ..
 template <typename T, bool PACKED, Mode MODE, int THREADS>
@@ -73,18 +73,22 @@ __global__ __launch_bounds__(THREADS) void k_scan_chunk(ScanParams p)
     const int count = static_cast<int>(w.t1 - w.t0);
     int ahead = 0;   // the token that the pointers of x, dt and z are at
     T xr[kTok], dr[kTok], zr[kTok];
-    const auto fetch = [&](int u) {
-        xr[u] = x.get(w.lane);
-        dr[u] = dt.get(w.lane);
-        if (gate) zr[u] = z.get(w.lane);
-        const bool more = ahead + 1 < count;   // (past the end: the last token again)
-        x.move(more);
-        dt.move(more);
-        if (gate) z.move(more);
-        ++ahead;
-    };
+    const auto fetch = [&]() {
 #pragma unroll
-    for (int u = 0; u < kTok; ++u) fetch(u);
+        for (int u = 0; u < kTok; ++u) {
+            xr[u] = x.get(w.lane);
+            dr[u] = dt.get(w.lane);
+            if (gate) zr[u] = z.get(w.lane);
+            const bool more = ++ahead < count;   // (at the end: the last token again)
+            x.move(more);
+            dt.move(more);
+            if (gate) z.move(more);
+        }
+    };
+    fetch();
+    Uniform<T, kSlice> bn, cn;   // the next token's B and C
+    bn.load(B);
+    if (kOut) cn.load(C);
     float* part = shared;
     for (int t = 0; t < count; t += kTok) {
         if (MODE == kMarks && t % kBwdTile == 0) {
@@ -95,7 +99,18 @@ __global__ __launch_bounds__(THREADS) void k_scan_chunk(ScanParams p)
                 for (int n = 0; n < kSlice; ++n) m[n * p.E] = h[n];
             }
         }
-        float xs[kTok], zs[kTok];   // several wavefronts: x and z for the end of the tile
+        float xv[kTok], d[kTok], zv[kTok];
+#pragma unroll
+        for (int u = 0; u < kTok; ++u) {
+            xv[u] = widen(xr[u]);
+            zv[u] = gate ? widen(zr[u]) : 0.f;
+            d[u] = widen(dr[u]) + bias;
+        }
+        fetch();   // the next tile's
+        if (p.softplus) {
+#pragma unroll
+            for (int u = 0; u < kTok; ++u) d[u] = softplus_hw(d[u]);
+        }
 #pragma unroll
         for (int u = 0; u < kTok; ++u) {
             if (t + u >= count) break;
@@ -105,22 +120,24 @@ __global__ __launch_bounds__(THREADS) void k_scan_chunk(ScanParams p)
                     load_states(p.init, p, unit, w.e, n0, h);
                 }
             }
-            const float xv = widen(xr[u]), zv = gate ? widen(zr[u]) : 0.f;
-            const float d = time_step(p, widen(dr[u]) + bias), in = d * xv;
-            fetch(u);
-            float b[kSlice], c[kSlice];
-            B.uniform(b);
-            B.move();
+            const float in = d[u] * xv[u];
+            Uniform<T, kSlice> b = bn, c = cn;
+            b.arrive();
+            if (kOut) c.arrive();
+            const bool more = t + u + 1 < count;
+            B.move(more);
+            bn.load(B);
             if (kOut) {
-                C.uniform(c);
-                C.move();
+                C.move(more);
+                cn.load(C);
             }
-            if (MODE == kStates) sum += d;
+            __builtin_amdgcn_sched_barrier(0);   // the loads stay in front of the token's arithmetic
+            if (MODE == kStates) sum += d[u];
             float y0 = 0.f, y1 = 0.f;
 #pragma unroll
             for (int n = 0; n < kSlice; n += 2) {
-                h[n] = fmaf(__builtin_amdgcn_exp2f(d * A2[n]), h[n], in * b[n]);
-                h[n + 1] = fmaf(__builtin_amdgcn_exp2f(d * A2[n + 1]), h[n + 1], in * b[n + 1]);
+                h[n] = fmaf(__builtin_amdgcn_exp2f(d[u] * A2[n]), h[n], in * b[n]);
+                h[n + 1] = fmaf(__builtin_amdgcn_exp2f(d[u] * A2[n + 1]), h[n + 1], in * b[n + 1]);
                 if (kOut) {
                     y0 = fmaf(h[n], c[n], y0);
                     y1 = fmaf(h[n + 1], c[n + 1], y1);
@@ -130,14 +147,12 @@ __global__ __launch_bounds__(THREADS) void k_scan_chunk(ScanParams p)
                 if (PACKED && p.fin && w.live && scan_ends<PACKED>(p, w.t0 + t + u))
                     store_states(p.fin, p, unit, w.e, n0, h);
                 if (kOne) {
-                    float v = fmaf(D, xv, y0 + y1);
-                    if (gate) v *= zv * sigmoid_hw(zv);
+                    float v = fmaf(D, xv[u], y0 + y1);
+                    if (gate) v *= zv[u] * sigmoid_hw(zv[u]);
                     if (w.live) y.put(w.lane, narrow<T>(v));
                     y.move();
                 } else {
                     part[(u * slices + slice) * 64 + col] = y0 + y1;
-                    xs[u] = xv;
-                    zs[u] = zv;
                 }
             }
         }
@@ -149,8 +164,8 @@ __global__ __launch_bounds__(THREADS) void k_scan_chunk(ScanParams p)
                 if (u % slices == slice) {
                     float v = 0.f;
                     for (int k = 0; k < slices; ++k) v += part[(u * slices + k) * 64 + col];
-                    v = fmaf(D, xs[u], v);
-                    if (gate) v *= zs[u] * sigmoid_hw(zs[u]);
+                    v = fmaf(D, xv[u], v);
+                    if (gate) v *= zv[u] * sigmoid_hw(zv[u]);
                     if (w.live) y.put(w.lane, narrow<T>(v));
                 }
                 y.move();
@@ -169,7 +184,7 @@ __global__ __launch_bounds__(THREADS) void k_scan_chunk(ScanParams p)
 
 // The scan over chunks: the states of each chunk (from zero) become the states
 // entering it.  A thread per batch row, state and channel.
-constexpr int kPassBatch = 8;
+constexpr int kPassBatch = 16;
 
 __global__ __launch_bounds__(256) void k_scan_pass(ScanParams p)
 {
@@ -294,10 +309,18 @@ ScanPlan scan_plan(int64_t b, int64_t T, int64_t E, int64_t N, int64_t G, bool b
 {
     ScanPlan w{};
     const int64_t tiles = G * scan_tiles(E, G), waves = b * tiles * (N / kSlice);
-    // Chunks: four wavefronts a SIMD (4,096), none shorter than 64 tokens.
-    int64_t S = (4096 + waves - 1) / waves;
-    const int64_t most = T / 64 > 1 ? T / 64 : 1;
-    if (S > most) S = most;
+    // Chunks: ten wavefronts a SIMD (10,240), where there are not one and a half
+    // (1,536) without: then the second pass costs more than idle SIMDs do (5,120
+    // channels of 1,024 tokens, us by batch rows, whole / in chunks: 12 rows, 960
+    // wavefronts, 536 / 451; 16 rows 679 / 571; 20 rows, 1,600, 689 / 771).  No chunk
+    // shorter than 16 sqrt(T / 1,024) tokens, the least of a chunk's own time and of
+    // the scan over the chunks' (1 x 777 x 5,120 float32: chunks of 16 tokens 61, 32
+    // 66, 64 74; 1 x 16,384 x 768: 32 171, 64 147, 128 172), and none below 64 tokens
+    // in all.
+    int64_t S = waves < 1536 ? 10240 / waves : 1, shortest = 16;
+    while (shortest * shortest * 4 < T) shortest *= 2;
+    if (S > T / shortest) S = T / shortest;
+    if (S < 1 || T < 64) S = 1;
     const int64_t unit = backward ? kBwdTile : kTok;
     w.L = ((T + S - 1) / S + unit - 1) / unit * unit;
     w.S = (T + w.L - 1) / w.L;
