@@ -139,9 +139,8 @@ __device__ __forceinline__ float sigmoid_hw(float v) { return __builtin_amdgcn_r
 // time step is.  -infinity gives 0, a NaN a NaN.
 constexpr float kAtanh0 = 2.f, kAtanh1 = 0.666663229f, kAtanh2 = 0.400245965f, kAtanh3 = 0.279651582f, kAtanh4 = 0.281577796f;   // times 2
 
-__device__ __forceinline__ float softplus_hw(float v)
+__device__ __forceinline__ float softplus_hw(float v, float u)   // u = exp_neg(|v|)
 {
-    const float u = exp_neg(fabsf(v));
     const float s = u * __builtin_amdgcn_rcpf(2.f + u), q = s * s;
     float r = fmaf(q, kAtanh4, kAtanh3);
     r = fmaf(r, q, kAtanh2);
@@ -149,6 +148,8 @@ __device__ __forceinline__ float softplus_hw(float v)
     r = fmaf(r, q, kAtanh0);
     return fmaf(s, r, __builtin_elementwise_maximum(v, 0.f));
 }
+
+__device__ __forceinline__ float softplus_hw(float v) { return softplus_hw(v, exp_neg(fabsf(v))); }
 
 __device__ __forceinline__ float widen(float v) { return v; }
 __device__ __forceinline__ float widen(uint16_t v) { return __uint_as_float(static_cast<uint32_t>(v) << 16); }

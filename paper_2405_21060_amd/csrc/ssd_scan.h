@@ -14,7 +14,7 @@ namespace ssd {
 
 constexpr int kSlice = 16;     // states a lane holds
 constexpr int kTok = 8;        // tokens whose loads are issued together
-constexpr int kBwdTile = 16;   // tokens per tile of the gradients
+constexpr int kBwdTile = 8;    // tokens per tile of the gradients
 
 // A wavefront's place: channel tile (64 channels of one group), chunk, batch row.
 struct ScanWork {

@@ -21,11 +21,14 @@
 namespace ssd {
 namespace {
 
-enum Mode { kOutput, kStates, kMarks };
+enum Mode { kOutput, kStates, kMarks, kBoth };
 
 // kOutput: y and final states.  kStates: each chunk's state from zero (from the
-// initial state in the first one) and its sum of dt.  kMarks: the states in front
-// of every tile of kBwdTile tokens, for the gradients.
+// initial state in the first one) and its sum of dt.  For the gradients, kBoth: that,
+// and the gradient of the state entering each chunk from the chunk's own outputs,
+// sum_t exp(A sum_{s <= t} dt_s) dy~_t C_t (walked forwards too, the product of the
+// decays so far kept: one exp2 serves both); kMarks: the states in front of every
+// tile of kBwdTile tokens.
 // Workgroup: a wavefront per 16 states, at most THREADS / 64 of them (the bound
 // says how many registers a lane may have).
 //
@@ -37,21 +40,29 @@ template <typename T, bool PACKED, Mode MODE, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_scan_chunk(ScanParams p)
 {
     extern __shared__ float shared[];   // kOutput with several wavefronts: [2][kTok][slices][64]
-    constexpr bool kOne = THREADS == 64, kOut = MODE == kOutput;
+    constexpr bool kOne = THREADS == 64, kOut = MODE == kOutput, kBack = MODE == kBoth;
     const int slice = kOne ? 0 : uniform(threadIdx.x >> 6);
     const int slices = kOne ? 1 : static_cast<int>(p.N / kSlice);
     const unsigned col = threadIdx.x & 63;
     const ScanWork w = scan_work(p, blockIdx.x);
     if (MODE == kStates && w.chunk == p.S - 1) return;   // no chunk after it
     const int n0 = slice * kSlice;
-    const bool gate = kOut && p.z;
+    const bool gate = (kOut || kBack) && p.z;
     Rows<const T> x(p.x, w.row * p.xb + w.t0 * p.xt + w.e0, p.xt);
     Rows<const T> dt(p.dt, w.row * p.db + w.t0 * p.dtt + w.e0, p.dtt);
     Rows<const T> z(gate ? p.z : p.x, gate ? w.row * p.zb + w.t0 * p.zt + w.e0 : 0, gate ? p.zt : 0);
     Rows<const T> B(p.B, w.row * p.bb + w.t0 * p.bt + w.g * p.N + n0, p.bt);
     Rows<const T> C(p.C, w.row * p.cb + w.t0 * p.ct + w.g * p.N + n0, p.ct);
-    Rows<T> y(p.y, (w.row * p.T + w.t0) * p.E + w.e0, p.E);
+    const int64_t out = (w.row * p.T + w.t0) * p.E + w.e0;
+    Rows<T> y(p.y, out, p.E);
+    Rows<const T> dy(kBack ? p.dy : p.x, kBack ? out : 0, kBack ? p.E : 0);
     float A2[kSlice], h[kSlice];
+    float cum[kSlice], r[kSlice];   // kBoth: decay since the chunk's start, gradient so far
+#pragma unroll
+    for (int n = 0; n < kSlice; ++n) {
+        cum[n] = 1.f;
+        r[n] = 0.f;
+    }
     load_states(p.A_log, p, 0, w.e, n0, A2);   // (E, N): the layout of one unit
 #pragma unroll
     for (int n = 0; n < kSlice; ++n) A2[n] = decay_rate(A2[n]);
@@ -61,7 +72,7 @@ __global__ __launch_bounds__(THREADS) void k_scan_chunk(ScanParams p)
     float* const st = p.states + ((w.row * p.S + w.chunk) * p.N + n0) * p.E + w.e;
     if (w.chunk == 0) {
         load_states(p.init, p, unit, w.e, n0, h);
-    } else if (MODE == kStates) {
+    } else if (MODE == kStates || kBack) {
 #pragma unroll
         for (int n = 0; n < kSlice; ++n) h[n] = 0.f;
     } else {
@@ -72,23 +83,35 @@ __global__ __launch_bounds__(THREADS) void k_scan_chunk(ScanParams p)
 
     const int count = static_cast<int>(w.t1 - w.t0);
     int ahead = 0;   // the token that the pointers of x, dt and z are at
-    T xr[kTok], dr[kTok], zr[kTok];
+    T xr[kTok], dr[kTok], zr[kTok], yr[kTok];
     const auto fetch = [&]() {
 #pragma unroll
         for (int u = 0; u < kTok; ++u) {
             xr[u] = x.get(w.lane);
             dr[u] = dt.get(w.lane);
             if (gate) zr[u] = z.get(w.lane);
+            if (kBack) yr[u] = dy.get(w.lane);
             const bool more = ++ahead < count;   // (at the end: the last token again)
             x.move(more);
             dt.move(more);
             if (gate) z.move(more);
+            if (kBack) dy.move(more);
         }
     };
     fetch();
     Uniform<T, kSlice> bn, cn;   // the next token's B and C
     bn.load(B);
-    if (kOut) cn.load(C);
+    if (kOut || kBack) cn.load(C);
+    // kBoth: the unit's sequence ends here; its final state's gradient counts too.
+    bool open = true;   // no sequence has ended in the chunk yet
+    const auto leave = [&]() {
+        if (!open) return;
+        open = false;
+        float f[kSlice];
+        load_states(p.dfin, p, unit, w.e, n0, f);
+#pragma unroll
+        for (int n = 0; n < kSlice; ++n) r[n] = fmaf(cum[n], f[n], r[n]);
+    };
     float* part = shared;
     for (int t = 0; t < count; t += kTok) {
         if (MODE == kMarks && t % kBwdTile == 0) {
@@ -99,12 +122,13 @@ __global__ __launch_bounds__(THREADS) void k_scan_chunk(ScanParams p)
                 for (int n = 0; n < kSlice; ++n) m[n * p.E] = h[n];
             }
         }
-        float xv[kTok], d[kTok], zv[kTok];
+        float xv[kTok], d[kTok], zv[kTok], dyg[kTok];
 #pragma unroll
         for (int u = 0; u < kTok; ++u) {
             xv[u] = widen(xr[u]);
             zv[u] = gate ? widen(zr[u]) : 0.f;
             d[u] = widen(dr[u]) + bias;
+            if (kBack) dyg[u] = gate ? widen(yr[u]) * zv[u] * sigmoid_hw(zv[u]) : widen(yr[u]);
         }
         fetch();   // the next tile's
         if (p.softplus) {
@@ -116,6 +140,9 @@ __global__ __launch_bounds__(THREADS) void k_scan_chunk(ScanParams p)
             if (t + u >= count) break;
             if (PACKED) {
                 if (w.t0 + t + u > 0 && scan_starts<PACKED>(p, w.t0 + t + u)) {
+                    // (from the first start behind the chunk's first token on, nothing
+                    // reaches back to the state entering it)
+                    if (kBack && t + u > 0) leave();
                     unit = scan_unit<PACKED>(p, w.row, w.t0 + t + u);
                     load_states(p.init, p, unit, w.e, n0, h);
                 }
@@ -123,36 +150,37 @@ __global__ __launch_bounds__(THREADS) void k_scan_chunk(ScanParams p)
             const float in = d[u] * xv[u];
             Uniform<T, kSlice> b = bn, c = cn;
             b.arrive();
-            if (kOut) c.arrive();
+            if (kOut || kBack) c.arrive();
             const bool more = t + u + 1 < count;
             B.move(more);
             bn.load(B);
-            if (kOut) {
+            if (kOut || kBack) {
                 C.move(more);
                 cn.load(C);
             }
             __builtin_amdgcn_sched_barrier(0);   // the loads stay in front of the token's arithmetic
-            if (MODE == kStates) sum += d[u];
-            float y0 = 0.f, y1 = 0.f;
+            if (MODE == kStates || kBack) sum += d[u];
+            float ys[2] = {0.f, 0.f};
 #pragma unroll
-            for (int n = 0; n < kSlice; n += 2) {
-                h[n] = fmaf(__builtin_amdgcn_exp2f(d[u] * A2[n]), h[n], in * b[n]);
-                h[n + 1] = fmaf(__builtin_amdgcn_exp2f(d[u] * A2[n + 1]), h[n + 1], in * b[n + 1]);
-                if (kOut) {
-                    y0 = fmaf(h[n], c[n], y0);
-                    y1 = fmaf(h[n + 1], c[n + 1], y1);
+            for (int n = 0; n < kSlice; ++n) {
+                const float a = __builtin_amdgcn_exp2f(d[u] * A2[n]);
+                h[n] = fmaf(a, h[n], in * b[n]);
+                if (kOut) ys[n % 2] = fmaf(h[n], c[n], ys[n % 2]);
+                if (kBack && (!PACKED || open)) {
+                    cum[n] *= a;
+                    r[n] = fmaf(cum[n], dyg[u] * c[n], r[n]);
                 }
             }
             if (kOut) {
                 if (PACKED && p.fin && w.live && scan_ends<PACKED>(p, w.t0 + t + u))
                     store_states(p.fin, p, unit, w.e, n0, h);
                 if (kOne) {
-                    float v = fmaf(D, xv[u], y0 + y1);
+                    float v = fmaf(D, xv[u], ys[0] + ys[1]);
                     if (gate) v *= zv[u] * sigmoid_hw(zv[u]);
                     if (w.live) y.put(w.lane, narrow<T>(v));
                     y.move();
                 } else {
-                    part[(u * slices + slice) * 64 + col] = y0 + y1;
+                    part[(u * slices + slice) * 64 + col] = ys[0] + ys[1];
                 }
             }
         }
@@ -175,9 +203,14 @@ __global__ __launch_bounds__(THREADS) void k_scan_chunk(ScanParams p)
         }
     }
     if (kOut && !PACKED && p.fin && w.live && w.t1 == p.T) store_states(p.fin, p, unit, w.e, n0, h);
-    if (MODE == kStates && w.live) {
+    if (kBack && scan_ends<PACKED>(p, w.t1 - 1)) leave();
+    if ((MODE == kStates || kBack) && w.live) {
+        float* const rs = p.rstates + (st - p.states);
 #pragma unroll
-        for (int n = 0; n < kSlice; ++n) st[n * p.E] = h[n];
+        for (int n = 0; n < kSlice; ++n) {
+            st[n * p.E] = h[n];
+            if (kBack) rs[n * p.E] = r[n];
+        }
         if (slice == 0) p.sums[(w.row * p.S + w.chunk) * p.E + w.e] = sum;
     }
 }
@@ -294,7 +327,7 @@ hipError_t chunks(const ScanParams& p, hipStream_t stream)
 hipError_t launch_scan_chunk_states(const ScanParams& p, bool bf16, bool marks, hipStream_t stream)
 {
     if (marks) return bf16 ? chunks<uint16_t, kMarks>(p, stream) : chunks<float, kMarks>(p, stream);
-    return bf16 ? chunks<uint16_t, kStates>(p, stream) : chunks<float, kStates>(p, stream);
+    return bf16 ? chunks<uint16_t, kBoth>(p, stream) : chunks<float, kBoth>(p, stream);
 }
 
 hipError_t launch_scan_pass(const ScanParams& p, hipStream_t stream)
@@ -335,9 +368,9 @@ ScanPlan scan_plan(int64_t b, int64_t T, int64_t E, int64_t N, int64_t G, bool b
     if (w.S > 1) {
         w.states = take(st);
         w.sums = take(b * w.S * E);
+        if (backward) w.rstates = take(st);
     }
     if (backward) {
-        w.rstates = take(st);
         w.marks = take(b * ((T + kBwdTile - 1) / kBwdTile) * N * E);
         w.pA = take(st);
         w.pD = take(b * w.S * 2 * E);
@@ -350,7 +383,7 @@ ScanPlan scan_plan(int64_t b, int64_t T, int64_t E, int64_t N, int64_t G, bool b
 hipError_t launch_scan_forward(const ScanParams& p, bool bf16, hipStream_t stream)
 {
     if (p.S > 1) {
-        hipError_t err = launch_scan_chunk_states(p, bf16, false, stream);
+        hipError_t err = bf16 ? chunks<uint16_t, kStates>(p, stream) : chunks<float, kStates>(p, stream);
         if (err == hipSuccess) err = launch_scan_pass(p, stream);
         if (err != hipSuccess) return err;
     }

@@ -8,15 +8,16 @@
 //     dz_t = dy_t (h_t . C_t + D x_t) silu'(z_t),   dD = sum_t dy~_t x_t
 //
 // Passes, each over chunks of tokens as in the forward: the chunks' states from
-// zero in both directions, a scan over the chunks in each, the states in front of
-// every tile of 16 tokens (the forward's kernel again), then k_scan_grad, which
-// takes its chunk's tiles in reverse: four states at a time, a tile's states are
-// computed again from its entering ones and kept, with the decays, in registers,
-// and then walked back.  The sums over channels for dB and dC run across the
-// lanes: 64 values, one after the other, are merged in a tree in which every
+// zero and the gradients of the states entering them, from zero too (one pass,
+// k_scan_chunk<kBoth>), a scan over the chunks in each direction, the states in
+// front of every tile of 8 tokens (the forward's kernel again), then k_scan_grad,
+// which takes its chunk's tiles in reverse: four states at a time, a tile's states
+// are computed again from its entering ones and kept, with the decays, in
+// registers, and then walked back.  The sums over channels for dB and dC run across
+// the lanes: the tile's 64 values of four states, one after the other, are merged in a tree in which every
 // level halves the lanes that a value is spread over, two instructions a value
 // where a sum of its own would take seven.  Sums over channel tiles, chunks and
-// rows are joined in a fixed order by k_scan_sums.
+// rows are joined in a fixed order by k_scan_sum_params and k_scan_sum_bc.
 //
 // Bound by vector arithmetic, like the forward.
 #include <type_traits>
@@ -29,60 +30,7 @@ namespace {
 
 __device__ __forceinline__ float silu_grad(float z, float s) { return s * fmaf(z, 1.f - s, 1.f); }
 
-// dy~ of a token.
-template <typename T>
-__device__ __forceinline__ float gated(float dy, const T* z, int64_t at)
-{
-    if (!z) return dy;
-    const float zv = widen(z[at]);
-    return dy * zv * sigmoid_hw(zv);
-}
-
-// Each chunk's gradient of the state entering it, from a zero gradient behind it
-// (from the final state's where a sequence ends).
-template <typename T, bool PACKED>
-__global__ void k_scan_rev(ScanParams p)
-{
-    const int slice = uniform(threadIdx.x >> 6), n0 = slice * kSlice;
-    const ScanWork w = scan_work(p, blockIdx.x);
-    const T* dt = static_cast<const T*>(p.dt) + w.row * p.db + w.e;
-    const T* z = p.z ? static_cast<const T*>(p.z) + w.row * p.zb + w.e : nullptr;
-    const T* C = static_cast<const T*>(p.C) + w.row * p.cb + w.g * p.N + n0;
-    const T* dy = static_cast<const T*>(p.dy) + w.row * p.T * p.E + w.e;
-    float A2[kSlice], g[kSlice];
-    load_states(p.A_log, p, 0, w.e, n0, A2);
-#pragma unroll
-    for (int n = 0; n < kSlice; ++n) {
-        A2[n] = decay_rate(A2[n]);
-        g[n] = 0.f;
-    }
-    const float bias = p.dt_bias ? p.dt_bias[w.e] : 0.f;
-    for (int64_t t = w.t1 - 1; t >= w.t0; t -= kTok) {
-        T dr[kTok], yr[kTok], zr[kTok];
-#pragma unroll
-        for (int u = 0; u < kTok; ++u) {
-            const int64_t at = t - u >= w.t0 ? t - u : w.t0;
-            dr[u] = dt[at * p.dtt];
-            yr[u] = dy[at * p.E];
-            if (z) zr[u] = z[at * p.zt];
-        }
-#pragma unroll
-        for (int u = 0; u < kTok; ++u) {
-            const int64_t at = t - u;
-            if (at < w.t0) break;
-            if (scan_ends<PACKED>(p, at)) load_states(p.dfin, p, scan_unit<PACKED>(p, w.row, at), w.e, n0, g);
-            const float d = time_step(p, widen(dr[u]) + bias), dyg = gated(widen(yr[u]), z ? zr : nullptr, u);
-            float c[kSlice];
-            uniform_row(C + at * p.ct, c);
-#pragma unroll
-            for (int n = 0; n < kSlice; ++n) g[n] = __builtin_amdgcn_exp2f(d * A2[n]) * fmaf(dyg, c[n], g[n]);
-        }
-    }
-    if (!w.live) return;
-    float* to = p.rstates + ((w.row * p.S + w.chunk) * p.N + n0) * p.E + w.e;
-#pragma unroll
-    for (int n = 0; n < kSlice; ++n) to[n * p.E] = g[n];
-}
+constexpr int kPassBatch = 16;
 
 // The scan over chunks, backwards: each chunk's own gradient becomes the gradient
 // behind it (of the state that it leaves to the next chunk).
@@ -95,17 +43,27 @@ __global__ __launch_bounds__(256) void k_scan_rev_pass(ScanParams p)
     float* st = p.rstates + (row * p.S * p.N + n) * p.E + e;
     const int64_t step = p.N * p.E;
     float g = 0.f;
-    for (int64_t c = p.S - 1; c >= 0; --c) {
-        const float own = st[c * step];
-        st[c * step] = g;
-        if (c == 0) break;
-        const float half = __builtin_amdgcn_exp2f(p.sums[(row * p.S + c) * p.E + e] * A2 * 0.5f);
-        const float through = g * half * half;
-        g = own;
-        const int64_t t0 = c * p.L, t1 = t0 + p.L < p.T ? t0 + p.L : p.T;
-        // (a sequence that ends in the chunk, its last token included, takes nothing from behind it)
-        const bool joined = t1 < p.T && (!p.seq_idx || (p.seq_idx[t0] == p.seq_idx[t1 - 1] && p.seq_idx[t1 - 1] == p.seq_idx[t1]));
-        if (joined) g += through;
+    for (int64_t c = p.S - 1; c >= 0; c -= kPassBatch) {
+        float own[kPassBatch], d[kPassBatch];
+#pragma unroll
+        for (int k = 0; k < kPassBatch; ++k) {
+            const int64_t at = c - k > 0 ? c - k : 0;
+            own[k] = st[at * step];
+            d[k] = p.sums[(row * p.S + at) * p.E + e];
+        }
+#pragma unroll
+        for (int k = 0; k < kPassBatch; ++k) {
+            const int64_t at = c - k;
+            if (at < 0) continue;
+            st[at * step] = g;
+            const float half = __builtin_amdgcn_exp2f(d[k] * A2 * 0.5f);
+            const float through = g * half * half;
+            const int64_t t0 = at * p.L, t1 = t0 + p.L < p.T ? t0 + p.L : p.T;
+            // (a sequence that ends in the chunk, its last token included, takes nothing from behind it)
+            const bool joined = t1 < p.T && (!p.seq_idx || (p.seq_idx[t0] == p.seq_idx[t1 - 1] &&
+                                                            p.seq_idx[t1 - 1] == p.seq_idx[t1]));
+            g = joined ? own[k] + through : own[k];
+        }
     }
 }
 
@@ -154,77 +112,132 @@ struct LaneSums {
     }
 };
 
-// k_scan_grad's tokens of a tile, from last to first: place I = 15 - token.
-template <int I, typename F>
+template <int I, int END, typename F>
 __device__ __forceinline__ void each(F&& f)
 {
-    if constexpr (I < kBwdTile) {
+    if constexpr (I < END) {
         f(std::integral_constant<int, I>{});
-        each<I + 1>(f);
+        each<I + 1, END>(f);
     }
 }
 
 constexpr int kQuad = 4;   // states taken at a time
+constexpr int kHalf = kBwdTile / 2;
+
+// B and C of half a tile's tokens, four states each.
+template <typename T>
+struct QuadRows {
+    Uniform<T, kQuad> b[kHalf], c[kHalf];
+
+    // from the rows' places on, at most `left` of them (then the last one again)
+    __device__ __forceinline__ void load(Rows<const T> B, Rows<const T> C, int left)
+    {
+#pragma unroll
+        for (int i = 0; i < kHalf; ++i) {
+            b[i].load(B);
+            c[i].load(C);
+            B.move(i + 1 < left);
+            C.move(i + 1 < left);
+        }
+    }
+    __device__ __forceinline__ void arrive()
+    {
+#pragma unroll
+        for (int i = 0; i < kHalf; ++i) {
+            b[i].arrive();
+            c[i].arrive();
+        }
+    }
+};
 
 // One wavefront: 64 channels of one chunk, its tiles from the last to the first.
 // Shared memory: the states' running gradients g and sums of dA, [2][N][64].
-template <typename T, bool PACKED>
-__global__ __launch_bounds__(64) void k_scan_grad(ScanParams p)
-{
-    extern __shared__ float shared[];
-    const int lane = threadIdx.x;
-    const ScanWork w = scan_work(p, blockIdx.x);
-    const int N = static_cast<int>(p.N);
-    float* const gs = shared + lane;
-    float* const as = shared + N * 64 + lane;
-    const int64_t tiles = (p.T + kBwdTile - 1) / kBwdTile;
-    const T* x = static_cast<const T*>(p.x) + w.row * p.xb + w.e;
-    const T* dt = static_cast<const T*>(p.dt) + w.row * p.db + w.e;
-    const T* z = p.z ? static_cast<const T*>(p.z) + w.row * p.zb + w.e : nullptr;
-    const T* B = static_cast<const T*>(p.B) + w.row * p.bb + w.g * p.N;
-    const T* C = static_cast<const T*>(p.C) + w.row * p.cb + w.g * p.N;
-    const int64_t out = w.row * p.T * p.E + w.e;
-    const T* dy = static_cast<const T*>(p.dy) + out;
-    const float* A_log = p.A_log + w.e * p.N;
-    const float bias = p.dt_bias ? p.dt_bias[w.e] : 0.f, D = p.D ? p.D[w.e] : 0.f;
-    // the chunk's rows of dB and dC: [token][group][2][N] of this channel tile
-    float* const bc = p.pBC + ((w.tile * p.b + w.row) * p.T * p.G + w.g) * 2 * p.N;
-    float sumD = 0.f, sumBias = 0.f;
-    {
-        const float* from = p.rstates + (w.row * p.S + w.chunk) * p.N * p.E + w.e;
-        for (int n = 0; n < N; ++n) {
-            gs[n * 64] = w.live ? from[n * p.E] : 0.f;
-            as[n * 64] = 0.f;
-        }
-    }
-    const int place = static_cast<int>(__brev(static_cast<unsigned>(lane)) >> 26);   // the value this lane gets
-    const int tok_of = kBwdTile - 1 - place / kQuad, n_of = place % kQuad;
+template <typename T, bool PACKED, bool GATE>
+struct GradTile {
+    const ScanParams& p;
+    const ScanWork& w;
+    float *gs, *as;
+    float bias, D, sumD, sumBias;
 
-    for (int64_t tile = (w.t1 - 1) / kBwdTile; tile * kBwdTile >= w.t0; --tile) {
-        const int64_t t0 = tile * kBwdTile;
-        const int count = static_cast<int>(w.t1 - t0 < kBwdTile ? w.t1 - t0 : kBwdTile);
-        float d[kBwdTile], xv[kBwdTile], dyg[kBwdTile], du[kBwdTile], sa[kBwdTile], ys[kBwdTile];
+    // FULL: all kBwdTile tokens are real.
+    template <bool FULL>
+    __device__ __forceinline__ void run(int64_t tile)
+    {
+        const int lane = threadIdx.x, N = static_cast<int>(p.N);
+        const int64_t t0 = tile * kBwdTile, out = (w.row * p.T + t0) * p.E + w.e0;
+        const int64_t tiles = (p.T + kBwdTile - 1) / kBwdTile;
+        const int count = FULL ? kBwdTile : static_cast<int>(w.t1 - t0);
+        float d[kBwdTile], slope[kBwdTile];   // dt and its derivative by dt_in
+        float xv[kBwdTile], dyg[kBwdTile], zd[kBwdTile], du[kBwdTile], sa[kBwdTile], ys[kBwdTile];
         unsigned starts = 0, ends = 0;   // bits: the token starts / ends a sequence
+        {
+            Rows<const T> x(p.x, w.row * p.xb + t0 * p.xt + w.e0, p.xt);
+            Rows<const T> dt(p.dt, w.row * p.db + t0 * p.dtt + w.e0, p.dtt);
+            Rows<const T> z(GATE ? p.z : p.x, GATE ? w.row * p.zb + t0 * p.zt + w.e0 : 0, GATE ? p.zt : 0);
+            Rows<const T> dy(p.dy, out, p.E);
+            T xr[kBwdTile], dr[kBwdTile], yr[kBwdTile], zr[kBwdTile];
 #pragma unroll
-        for (int u = 0; u < kBwdTile; ++u) {
-            const int64_t at = u < count ? t0 + u : w.t1 - 1;
-            xv[u] = widen(x[at * p.xt]);
-            d[u] = widen(dt[at * p.dtt]);
-            dyg[u] = w.live && u < count ? gated(widen(dy[at * p.E]), z, at * p.zt) : 0.f;
-            du[u] = sa[u] = ys[u] = 0.f;
-            if (u < count) {
-                if (scan_starts<PACKED>(p, at)) starts |= 1u << u;
-                if (scan_ends<PACKED>(p, at)) ends |= 1u << u;
+            for (int u = 0; u < kBwdTile; ++u) {
+                xr[u] = x.get(w.lane);
+                dr[u] = dt.get(w.lane);
+                yr[u] = dy.get(w.lane);
+                if (GATE) zr[u] = z.get(w.lane);
+                const bool more = FULL || u + 1 < count;   // (at the end: the last token again)
+                if (u + 1 == kBwdTile) break;
+                x.move(more);
+                dt.move(more);
+                dy.move(more);
+                if (GATE) z.move(more);
+            }
+#pragma unroll
+            for (int u = 0; u < kBwdTile; ++u) {
+                xv[u] = widen(xr[u]);
+                const float v = widen(dr[u]) + bias, dyv = w.live ? widen(yr[u]) : 0.f;
+                d[u] = v;
+                slope[u] = 1.f;
+                if (p.softplus) {
+                    const float e = exp_neg(fabsf(v));
+                    d[u] = softplus_hw(v, e);
+                    slope[u] = (v >= 0.f ? 1.f : e) * __builtin_amdgcn_rcpf(1.f + e);
+                }
+                dyg[u] = dyv;
+                if (GATE) {
+                    const float zv = widen(zr[u]), s = sigmoid_hw(zv);
+                    dyg[u] = dyv * zv * s;
+                    zd[u] = dyv * silu_grad(zv, s);
+                }
+                du[u] = sa[u] = ys[u] = 0.f;
+                if (PACKED && (FULL || u < count)) {
+                    if (scan_starts<PACKED>(p, t0 + u)) starts |= 1u << u;
+                    if (scan_ends<PACKED>(p, t0 + u)) ends |= 1u << u;
+                }
+            }
+            if (!PACKED) {
+                starts = t0 == 0 ? 1u : 0u;
+                ends = t0 + count == p.T ? 1u << (count - 1) : 0u;
             }
         }
-#pragma unroll
-        for (int u = 0; u < kBwdTile; ++u)   // (a token past the end: no decay, no input)
-            d[u] = u < count ? time_step(p, d[u] + bias) : 0.f;
+        Rows<const T> B0(p.B, w.row * p.bb + t0 * p.bt + w.g * p.N, p.bt), B1 = B0;
+        Rows<const T> C0(p.C, w.row * p.cb + t0 * p.ct + w.g * p.N, p.ct), C1 = C0;
+        const bool second = FULL || count > kHalf;   // there are tokens in the tile's second half
+        B1.p += second ? static_cast<int64_t>(kHalf) * p.bt : 0;
+        C1.p += second ? static_cast<int64_t>(kHalf) * p.ct : 0;
+        running(B1.p);
+        running(C1.p);
+        const int left0 = FULL ? kHalf : count, left1 = FULL ? kHalf : second ? count - kHalf : 1;
+        const float* m = p.marks + (w.row * tiles + tile) * p.N * p.E + w.e;
+        const float* A_log = p.A_log + w.e * p.N;
+        // the value that this lane gets of the 64: token, dB or dC, state
+        const int place = static_cast<int>(__brev(static_cast<unsigned>(lane)) >> 26);
+        const int tok = kBwdTile - 1 - place / (2 * kQuad);
+        float* to = p.pBC + (((w.tile * p.b + w.row) * p.T + t0 + tok) * p.G + w.g) * 2 * p.N +
+                    (place / kQuad % 2) * p.N + place % kQuad;
 
         for (int q = 0; q < N; q += kQuad) {
             float A2[kQuad], h[kQuad], g[kQuad], dA[kQuad];
             float hb[kBwdTile][kQuad], a[kBwdTile][kQuad];   // state before each token, its decay
-            const float* m = p.marks + ((w.row * tiles + tile) * p.N + q) * p.E + w.e;
+            QuadRows<T> lo, hi;
+            lo.load(B0, C0, left0);
 #pragma unroll
             for (int n = 0; n < kQuad; ++n) {
                 A2[n] = decay_rate(A_log[q + n]);
@@ -232,120 +245,162 @@ __global__ __launch_bounds__(64) void k_scan_grad(ScanParams p)
                 g[n] = gs[(q + n) * 64];
                 dA[n] = as[(q + n) * 64];
             }
-#pragma unroll
-            for (int u = 0; u < kBwdTile; ++u) {
-                const int64_t at = u < count ? t0 + u : w.t1 - 1;
-                if (starts >> u & 1) {
-                    const int64_t unit = scan_unit<PACKED>(p, w.row, at);
+            lo.arrive();
+            hi.load(B1, C1, left1);
+            __builtin_amdgcn_sched_barrier(0);
+            each<0, kBwdTile>([&](auto i) {
+                constexpr int u = decltype(i)::value, k = u % kHalf;
+                if constexpr (u == kHalf) hi.arrive();
+                if (!FULL && u >= count) return;
+                if (PACKED && (starts >> u & 1)) {
+                    const int64_t unit = scan_unit<PACKED>(p, w.row, t0 + u);
 #pragma unroll
                     for (int n = 0; n < kQuad; ++n) h[n] = p.init ? p.init[(unit * p.E + w.e) * p.N + q + n] : 0.f;
                 }
-                float b[kQuad], c[kQuad];
-                uniform_row(B + at * p.bt + q, b);
-                uniform_row(C + at * p.ct + q, c);
-                const float in = u < count ? d[u] * xv[u] : 0.f;
+                const QuadRows<T>& bc = u < kHalf ? lo : hi;
+                const float in = d[u] * xv[u];
 #pragma unroll
                 for (int n = 0; n < kQuad; ++n) {
                     a[u][n] = __builtin_amdgcn_exp2f(d[u] * A2[n]);
                     hb[u][n] = h[n];
-                    h[n] = fmaf(a[u][n], h[n], in * b[n]);
-                    if (p.dz) ys[u] = fmaf(h[n], c[n], ys[u]);
+                    h[n] = fmaf(a[u][n], h[n], in * bc.b[k][n]);
+                    if (GATE) ys[u] = fmaf(h[n], bc.c[k][n], ys[u]);
                 }
-            }
-            LaneSums sB, sC;
-            each<0>([&](auto i) {
-                constexpr int I = decltype(i)::value, u = kBwdTile - 1 - I;
-                const int64_t at = u < count ? t0 + u : w.t1 - 1;
-                float b[kQuad], c[kQuad];
-                uniform_row(B + at * p.bt + q, b);
-                uniform_row(C + at * p.ct + q, c);
-                const float in = u < count ? d[u] * xv[u] : 0.f;
+            });
+            lo.load(B0, C0, left0);   // (again, for the way back)
+            __builtin_amdgcn_sched_barrier(0);
+            LaneSums sums;
+            each<0, kBwdTile>([&](auto i) {
+                constexpr int I = decltype(i)::value, u = kBwdTile - 1 - I, k = u % kHalf;
+                constexpr int first = I * 2 * kQuad;
+                if constexpr (u == kHalf - 1) lo.arrive();
+                if (!FULL && u >= count) {
+                    each<0, 2 * kQuad>([&](auto n) { sums.template put<first + decltype(n)::value>(0.f, lane); });
+                    return;
+                }
+                const QuadRows<T>& bc = u < kHalf ? lo : hi;
+                const float in = d[u] * xv[u];
                 if (ends >> u & 1) {
-                    const int64_t unit = scan_unit<PACKED>(p, w.row, at);
+                    const int64_t unit = scan_unit<PACKED>(p, w.row, t0 + u);
 #pragma unroll
                     for (int n = 0; n < kQuad; ++n)
                         g[n] = p.dfin && w.live ? p.dfin[(unit * p.E + w.e) * p.N + q + n] : 0.f;
                 }
-                const auto one = [&](auto k) {
-                    constexpr int n = decltype(k)::value;
-                    const float hn = fmaf(a[u][n], hb[u][n], in * b[n]);   // the state after the token
-                    g[n] = fmaf(dyg[u], c[n], g[n]);
-                    sC.template put<I * kQuad + n>(dyg[u] * hn, lane);
-                    sB.template put<I * kQuad + n>(w.live ? g[n] * in : 0.f, lane);
-                    du[u] = fmaf(g[n], b[n], du[u]);
+#pragma unroll
+                for (int n = 0; n < kQuad; ++n) {
+                    g[n] = fmaf(dyg[u], bc.c[k][n], g[n]);
+                    du[u] = fmaf(g[n], bc.b[k][n], du[u]);
+                }
+                each<0, kQuad>([&](auto n) { sums.template put<first + decltype(n)::value>(g[n] * in, lane); });
+                each<0, kQuad>([&](auto j) {
+                    constexpr int n = decltype(j)::value;
+                    // the state after the token: that before the next one, if no sequence starts there
+                    float after;
+                    if constexpr (PACKED || !FULL)
+                        after = fmaf(a[u][n], hb[u][n], in * bc.b[k][n]);
+                    else
+                        after = u + 1 < kBwdTile ? hb[u + 1 < kBwdTile ? u + 1 : u][n] : h[n];
+                    sums.template put<first + kQuad + n>(dyg[u] * after, lane);
+                });
+#pragma unroll
+                for (int n = 0; n < kQuad; ++n) {
                     g[n] *= a[u][n];
                     const float e = g[n] * hb[u][n];
                     sa[u] = fmaf(e, A2[n], sa[u]);
                     dA[n] = fmaf(e, d[u], dA[n]);
-                };
-                one(std::integral_constant<int, 0>{});
-                one(std::integral_constant<int, 1>{});
-                one(std::integral_constant<int, 2>{});
-                one(std::integral_constant<int, 3>{});
-                if (starts >> u & 1) {
-                    if (p.dinit && w.live) {
-                        const int64_t unit = scan_unit<PACKED>(p, w.row, at);
+                }
+                if ((PACKED || u == 0) && (starts >> u & 1) && p.dinit && w.live) {
+                    const int64_t unit = scan_unit<PACKED>(p, w.row, t0 + u);
 #pragma unroll
-                        for (int n = 0; n < kQuad; ++n) p.dinit[(unit * p.E + w.e) * p.N + q + n] = g[n];
-                    }
+                    for (int n = 0; n < kQuad; ++n) p.dinit[(unit * p.E + w.e) * p.N + q + n] = g[n];
                 }
             });
-            if (tok_of < count) {
-                float* to = bc + (t0 + tok_of) * p.G * 2 * p.N + q + n_of;
-                to[0] = sB.out;
-                to[p.N] = sC.out;
-            }
+            if (FULL || tok < count) *to = sums.out;
 #pragma unroll
             for (int n = 0; n < kQuad; ++n) {
                 gs[(q + n) * 64] = g[n];
                 as[(q + n) * 64] = dA[n];
             }
+            B0.p += kQuad;
+            C0.p += kQuad;
+            B1.p += kQuad;
+            C1.p += kQuad;
+            m += kQuad * p.E;
+            to += kQuad;
         }
+
+        Rows<T> dx(p.dx, out, p.E), ddt(p.ddt, out, p.E), dz(GATE ? p.dz : p.dx, out, p.E);
 #pragma unroll
         for (int u = 0; u < kBwdTile; ++u) {
-            const int64_t at = u < count ? t0 + u : w.t1 - 1, o = out + at * p.E;
-            const float dx = fmaf(d[u], du[u], D * dyg[u]);
-            float dd = fmaf(xv[u], du[u], sa[u] * 0.69314718f);   // (A2 is A log2(e))
-            if (p.softplus) dd *= sigmoid_hw(widen(dt[at * p.dtt]) + bias);
-            if (u < count) {
+            if (FULL || u < count) {
+                const float dd = fmaf(xv[u], du[u], sa[u] * 0.69314718f) * slope[u];   // (A2 is A log2(e))
                 sumD = fmaf(dyg[u], xv[u], sumD);
                 sumBias += dd;
-            }
-            if (w.live && u < count) {
-                static_cast<T*>(p.dx)[o] = narrow<T>(dx);
-                static_cast<T*>(p.ddt)[o] = narrow<T>(dd);
-                if (p.dz) {
-                    const float zv = widen(z[at * p.zt]), s = sigmoid_hw(zv);
-                    static_cast<T*>(p.dz)[o] = narrow<T>(widen(dy[at * p.E]) * fmaf(D, xv[u], ys[u]) * silu_grad(zv, s));
+                if (w.live) {
+                    dx.put(w.lane, narrow<T>(fmaf(d[u], du[u], D * dyg[u])));
+                    ddt.put(w.lane, narrow<T>(dd));
+                    if (GATE) dz.put(w.lane, narrow<T>(zd[u] * fmaf(D, xv[u], ys[u])));
                 }
+                dx.move();
+                ddt.move();
+                if (GATE) dz.move();
             }
         }
     }
+};
+
+template <typename T, bool PACKED, bool GATE>
+__global__ __launch_bounds__(64, 2) void k_scan_grad(ScanParams p)
+{
+    extern __shared__ float shared[];
+    const int lane = threadIdx.x, N = static_cast<int>(p.N);
+    const ScanWork w = scan_work(p, blockIdx.x);
+    GradTile<T, PACKED, GATE> g{p, w, shared + lane, shared + N * 64 + lane,
+                                p.dt_bias ? p.dt_bias[w.e] : 0.f, p.D ? p.D[w.e] : 0.f, 0.f, 0.f};
+    const float* from = p.rstates + (w.row * p.S + w.chunk) * p.N * p.E + w.e;
+    for (int n = 0; n < N; ++n) {
+        g.gs[n * 64] = w.live && p.S > 1 ? from[n * p.E] : 0.f;
+        g.as[n * 64] = 0.f;
+    }
+    int64_t tile = (w.t1 - 1) / kBwdTile;
+    if (w.t1 - tile * kBwdTile < kBwdTile) g.template run<false>(tile--);
+    for (; tile * kBwdTile >= w.t0; --tile) g.template run<true>(tile);
     if (!w.live) return;
     const int64_t rc = w.row * p.S + w.chunk;
-    for (int n = 0; n < N; ++n) p.pA[(rc * p.N + n) * p.E + w.e] = as[n * 64];
-    p.pD[rc * 2 * p.E + w.e] = sumD;
-    p.pD[(rc * 2 + 1) * p.E + w.e] = sumBias;
+    for (int n = 0; n < N; ++n) p.pA[(rc * p.N + n) * p.E + w.e] = g.as[n * 64];
+    p.pD[rc * 2 * p.E + w.e] = g.sumD;
+    p.pD[(rc * 2 + 1) * p.E + w.e] = g.sumBias;
 }
 
-// dA_log, dD and ddt_bias: sums over rows and chunks, in order.
-__global__ __launch_bounds__(256) void k_scan_sum_params(ScanParams p)
+// dA_log, dD and ddt_bias: sums over rows and chunks, eight interleaved ones a
+// column joined at the end.
+constexpr int kSumLanes = 8, kSumCols = 32;
+
+__global__ __launch_bounds__(kSumLanes * kSumCols) void k_scan_sum_params(ScanParams p)
 {
-    const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, ne = p.N * p.E, parts = p.b * p.S;
-    if (i < ne) {
+    __shared__ float part[kSumLanes][kSumCols + 1];
+    const int col = threadIdx.x % kSumCols, lane = threadIdx.x / kSumCols;
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * kSumCols + col, ne = p.N * p.E, parts = p.b * p.S;
+    const bool first = i < ne;   // (N E is a multiple of 16: a column of dA or one of dD, ddt_bias)
+    const float* from = first ? p.pA + i : p.pD + (i - ne);
+    const int64_t step = first ? ne : 2 * p.E;
+    float v = 0.f;
+    if (i < ne + 2 * p.E)
+        for (int64_t k = lane; k < parts; k += kSumLanes) v += from[k * step];
+    part[lane][col] = v;
+    __syncthreads();
+    if (lane != 0 || i >= ne + 2 * p.E) return;
+    v = 0.f;
+#pragma unroll
+    for (int k = 0; k < kSumLanes; ++k) v += part[k][col];
+    if (first) {
         const int64_t n = i / p.E, e = i - n * p.E;
-        float v = 0.f;
-        for (int64_t k = 0; k < parts; ++k) v += p.pA[k * ne + i];
-        p.dA_log[e * p.N + n] = v * -expf(p.A_log[e * p.N + n]);
+        p.dA_log[e * p.N + n] = v * (decay_rate(p.A_log[e * p.N + n]) * 0.69314718f);
         return;
     }
     const int64_t j = i - ne;
-    if (j >= 2 * p.E) return;
     float* to = j < p.E ? p.dD : p.ddt_bias;
-    if (!to) return;
-    float v = 0.f;
-    for (int64_t k = 0; k < parts; ++k) v += p.pD[k * 2 * p.E + j];
-    to[j < p.E ? j : j - p.E] = v;
+    if (to) to[j < p.E ? j : j - p.E] = v;
 }
 
 // dB and dC: sums over a group's channel tiles, in order.
@@ -361,30 +416,36 @@ __global__ __launch_bounds__(256) void k_scan_sum_bc(ScanParams p, int64_t block
     to[tg * p.N + (n < p.N ? n : n - p.N)] = narrow<T>(v);
 }
 
+template <typename T, bool PACKED, bool GATE>
+hipError_t grad(const ScanParams& p, int64_t units, hipStream_t stream)
+{
+    const size_t lds = 2 * static_cast<size_t>(p.N) * 64 * sizeof(float);
+    if (lds > 65536) {   // (N > 128) beyond the default limit
+        const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_scan_grad<T, PACKED, GATE>),
+                                                   hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));
+        if (err != hipSuccess) return err;
+    }
+    hipLaunchKernelGGL((k_scan_grad<T, PACKED, GATE>), dim3(static_cast<unsigned>(units)), dim3(64), lds, stream, p);
+    return hipGetLastError();
+}
+
 template <typename T, bool PACKED>
 hipError_t run(const ScanParams& p, hipStream_t stream)
 {
     const int64_t units = p.b * p.S * p.G * scan_tiles(p.E, p.G);
-    const int64_t sums = (p.N * p.E + 2 * p.E + 255) / 256, bc = (p.b * p.T * p.G * 2 * p.N + 255) / 256;
+    const int64_t sums = (p.N * p.E + 2 * p.E + kSumCols - 1) / kSumCols, bc = (p.b * p.T * p.G * 2 * p.N + 255) / 256;
     const int64_t pass = (p.b * p.N * p.E + 255) / 256;
     if (units > kMaxGrid || sums > kMaxGrid || bc > kMaxGrid || pass > kMaxGrid) return hipErrorInvalidConfiguration;
-    const unsigned threads = 64 * static_cast<unsigned>(p.N / kSlice);
     if (p.S > 1) {
         if (hipError_t err = launch_scan_chunk_states(p, sizeof(T) == 2, false, stream); err != hipSuccess) return err;
         if (hipError_t err = launch_scan_pass(p, stream); err != hipSuccess) return err;
+        hipLaunchKernelGGL(k_scan_rev_pass, dim3(static_cast<unsigned>(pass)), dim3(256), 0, stream, p);
     }
     if (hipError_t err = launch_scan_chunk_states(p, sizeof(T) == 2, true, stream); err != hipSuccess) return err;
-    hipLaunchKernelGGL((k_scan_rev<T, PACKED>), dim3(static_cast<unsigned>(units)), dim3(threads), 0, stream, p);
-    hipLaunchKernelGGL(k_scan_rev_pass, dim3(static_cast<unsigned>(pass)), dim3(256), 0, stream, p);
-    if (hipError_t err = hipGetLastError(); err != hipSuccess) return err;
-    const size_t lds = 2 * static_cast<size_t>(p.N) * 64 * sizeof(float);
-    if (lds > 65536) {   // (N > 128) beyond the default limit
-        const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_scan_grad<T, PACKED>),
-                                                   hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));
-        if (err != hipSuccess) return err;
-    }
-    hipLaunchKernelGGL((k_scan_grad<T, PACKED>), dim3(static_cast<unsigned>(units)), dim3(64), lds, stream, p);
-    hipLaunchKernelGGL(k_scan_sum_params, dim3(static_cast<unsigned>(sums)), dim3(256), 0, stream, p);
+    if (hipError_t err = p.z ? grad<T, PACKED, true>(p, units, stream) : grad<T, PACKED, false>(p, units, stream);
+        err != hipSuccess)
+        return err;
+    hipLaunchKernelGGL(k_scan_sum_params, dim3(static_cast<unsigned>(sums)), dim3(kSumLanes * kSumCols), 0, stream, p);
     hipLaunchKernelGGL((k_scan_sum_bc<T>), dim3(static_cast<unsigned>(bc)), dim3(256), 0, stream, p,
                        scan_tiles(p.E, p.G));
     return hipGetLastError();
