@@ -59,7 +59,8 @@ struct ScanParams {
     void *dx, *ddt, *dB, *dC, *dz;
     float *dA_log, *dD, *ddt_bias, *dinit;
     float* rstates;                      // (b, S, N, E) reverse chunk states
-    float* marks;                        // states at every kBwdTile tokens (b, tiles, N, E)
+    float* marks;                        // states at every tile of tokens (b, tiles, N, E), and
+    float* marksums;                     // sums of dt (b, tiles, E), both from the chunk's start
     float* pA;                           // (b S, N, E) partial sums of dA
     float* pD;                           // (b S, 2, E) of dD, ddt_bias
     float* pBC;                          // (channel blocks, b, T, 2, N) of dB, dC
@@ -67,7 +68,7 @@ struct ScanParams {
 
 struct ScanPlan {
     int64_t S, L;
-    size_t states, sums, rstates, marks, pA, pD, pBC, total;   // byte offsets
+    size_t states, sums, rstates, marks, marksums, pA, pD, pBC, total;   // byte offsets
     int64_t cblocks;   // channel blocks of the gradients
 };
 

@@ -147,6 +147,7 @@ void place(const ssd::ScanPlan& w, void* workspace, ssd::ScanParams* p)
     p->sums = at(w.sums);
     p->rstates = at(w.rstates);
     p->marks = at(w.marks);
+    p->marksums = at(w.marksums);
     p->pA = at(w.pA);
     p->pD = at(w.pD);
     p->pBC = at(w.pBC);

@@ -166,7 +166,7 @@ __device__ __forceinline__ float decay_rate(float a_log) { return exp_neg(-a_log
 
 __device__ __forceinline__ float time_step(const ScanParams& p, float v) { return p.softplus ? softplus_hw(v) : v; }
 
-hipError_t launch_scan_chunk_states(const ScanParams& p, bool bf16, bool marks, hipStream_t stream);
+hipError_t launch_scan_both(const ScanParams& p, bool bf16, hipStream_t stream);
 hipError_t launch_scan_pass(const ScanParams& p, hipStream_t stream);
 
 }  // namespace ssd

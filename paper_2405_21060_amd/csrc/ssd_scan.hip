@@ -21,14 +21,14 @@
 namespace ssd {
 namespace {
 
-enum Mode { kOutput, kStates, kMarks, kBoth };
+enum Mode { kOutput, kStates, kBoth };
 
 // kOutput: y and final states.  kStates: each chunk's state from zero (from the
 // initial state in the first one) and its sum of dt.  For the gradients, kBoth: that,
 // and the gradient of the state entering each chunk from the chunk's own outputs,
 // sum_t exp(A sum_{s <= t} dt_s) dy~_t C_t (walked forwards too, the product of the
-// decays so far kept: one exp2 serves both); kMarks: the states in front of every
-// tile of kBwdTile tokens.
+// decays so far kept: one exp2 serves both), and in front of every tile of kBwdTile
+// tokens the state, from zero as it is, and the sum of dt since the chunk's start.
 // Workgroup: a wavefront per 16 states, at most THREADS / 64 of them (the bound
 // says how many registers a lane may have).
 //
@@ -114,13 +114,13 @@ __global__ __launch_bounds__(THREADS) void k_scan_chunk(ScanParams p)
     };
     float* part = shared;
     for (int t = 0; t < count; t += kTok) {
-        if (MODE == kMarks && t % kBwdTile == 0) {
-            const int64_t tile = (w.t0 + t) / kBwdTile, tiles = (p.T + kBwdTile - 1) / kBwdTile;
-            float* m = p.marks + ((w.row * tiles + tile) * p.N + n0) * p.E + w.e;
-            if (w.live) {
+        static_assert(kTok == kBwdTile, "a mark in front of every tile");
+        if (kBack && w.live) {
+            const int64_t tile = w.row * ((p.T + kBwdTile - 1) / kBwdTile) + (w.t0 + t) / kBwdTile;
+            float* m = p.marks + (tile * p.N + n0) * p.E + w.e;
 #pragma unroll
-                for (int n = 0; n < kSlice; ++n) m[n * p.E] = h[n];
-            }
+            for (int n = 0; n < kSlice; ++n) m[n * p.E] = h[n];
+            if (slice == 0) p.marksums[tile * p.E + w.e] = sum;
         }
         float xv[kTok], d[kTok], zv[kTok], dyg[kTok];
 #pragma unroll
@@ -204,7 +204,7 @@ __global__ __launch_bounds__(THREADS) void k_scan_chunk(ScanParams p)
     }
     if (kOut && !PACKED && p.fin && w.live && w.t1 == p.T) store_states(p.fin, p, unit, w.e, n0, h);
     if (kBack && scan_ends<PACKED>(p, w.t1 - 1)) leave();
-    if ((MODE == kStates || kBack) && w.live) {
+    if ((MODE == kStates || kBack) && w.live && p.S > 1) {
         float* const rs = p.rstates + (st - p.states);
 #pragma unroll
         for (int n = 0; n < kSlice; ++n) {
@@ -324,9 +324,8 @@ hipError_t chunks(const ScanParams& p, hipStream_t stream)
 
 }  // namespace
 
-hipError_t launch_scan_chunk_states(const ScanParams& p, bool bf16, bool marks, hipStream_t stream)
+hipError_t launch_scan_both(const ScanParams& p, bool bf16, hipStream_t stream)
 {
-    if (marks) return bf16 ? chunks<uint16_t, kMarks>(p, stream) : chunks<float, kMarks>(p, stream);
     return bf16 ? chunks<uint16_t, kBoth>(p, stream) : chunks<float, kBoth>(p, stream);
 }
 
@@ -342,7 +341,9 @@ ScanPlan scan_plan(int64_t b, int64_t T, int64_t E, int64_t N, int64_t G, bool b
 {
     ScanPlan w{};
     const int64_t tiles = G * scan_tiles(E, G), waves = b * tiles * (N / kSlice);
-    // Chunks: ten wavefronts a SIMD (10,240), where there are not one and a half
+    // Chunks: ten wavefronts a SIMD (10,240; gradients 6,144, three rounds of the two
+    // that a SIMD holds of k_scan_grad and two of the three of k_scan_chunk<kBoth>: 8 x
+    // 2,048 x 1,536 591 us, 4,096 wavefronts 628, 8,256 648), where there are not one and a half
     // (1,536) without: then the second pass costs more than idle SIMDs do (5,120
     // channels of 1,024 tokens, us by batch rows, whole / in chunks: 12 rows, 960
     // wavefronts, 536 / 451; 16 rows 679 / 571; 20 rows, 1,600, 689 / 771).  No chunk
@@ -350,7 +351,7 @@ ScanPlan scan_plan(int64_t b, int64_t T, int64_t E, int64_t N, int64_t G, bool b
     // the scan over the chunks' (1 x 777 x 5,120 float32: chunks of 16 tokens 61, 32
     // 66, 64 74; 1 x 16,384 x 768: 32 171, 64 147, 128 172), and none below 64 tokens
     // in all.
-    int64_t S = waves < 1536 ? 10240 / waves : 1, shortest = 16;
+    int64_t S = waves < 1536 ? (backward ? 6144 : 10240) / waves : 1, shortest = 16;
     while (shortest * shortest * 4 < T) shortest *= 2;
     if (S > T / shortest) S = T / shortest;
     if (S < 1 || T < 64) S = 1;
@@ -372,6 +373,7 @@ ScanPlan scan_plan(int64_t b, int64_t T, int64_t E, int64_t N, int64_t G, bool b
     }
     if (backward) {
         w.marks = take(b * ((T + kBwdTile - 1) / kBwdTile) * N * E);
+        w.marksums = take(b * ((T + kBwdTile - 1) / kBwdTile) * E);
         w.pA = take(st);
         w.pD = take(b * w.S * 2 * E);
         w.pBC = take(w.cblocks * b * T * G * 2 * N);

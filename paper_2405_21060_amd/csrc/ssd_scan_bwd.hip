@@ -8,10 +8,11 @@
 //     dz_t = dy_t (h_t . C_t + D x_t) silu'(z_t),   dD = sum_t dy~_t x_t
 //
 // Passes, each over chunks of tokens as in the forward: the chunks' states from
-// zero and the gradients of the states entering them, from zero too (one pass,
-// k_scan_chunk<kBoth>), a scan over the chunks in each direction, the states in
-// front of every tile of 8 tokens (the forward's kernel again), then k_scan_grad,
-// which takes its chunk's tiles in reverse: four states at a time, a tile's states
+// zero, also in front of every tile of 8 tokens, and the gradients of the states
+// entering them, from zero too (one pass, k_scan_chunk<kBoth>), a scan over the
+// chunks in each direction, then k_scan_grad, which takes its chunk's tiles in
+// reverse: the state in front of a tile is the one kept for it and what is left of
+// the one entering the chunk; four states at a time, a tile's states
 // are computed again from its entering ones and kept, with the decays, in
 // registers, and then walked back.  The sums over channels for dB and dC run across
 // the lanes: the tile's 64 values of four states, one after the other, are merged in a tree in which every
@@ -122,6 +123,7 @@ __device__ __forceinline__ void each(F&& f)
 }
 
 constexpr int kQuad = 4;   // states taken at a time
+
 constexpr int kHalf = kBwdTile / 2;
 
 // B and C of half a tile's tokens, four states each.
@@ -150,231 +152,276 @@ struct QuadRows {
     }
 };
 
-// One wavefront: 64 channels of one chunk, its tiles from the last to the first.
-// Shared memory: the states' running gradients g and sums of dA, [2][N][64].
-template <typename T, bool PACKED, bool GATE>
-struct GradTile {
-    const ScanParams& p;
-    const ScanWork& w;
-    float *gs, *as;
-    float bias, D, sumD, sumBias;
+template <bool FIRST, typename R>
+__device__ __forceinline__ const R& half(const R& lo, const R& hi)
+{
+    if constexpr (FIRST)
+        return lo;
+    else
+        return hi;
+}
 
-    // FULL: all kBwdTile tokens are real.
-    template <bool FULL>
-    __device__ __forceinline__ void run(int64_t tile)
+// A tile of k_scan_grad (FULL: all its kBwdTile tokens are real); adds to the
+// channel's sums of dD and ddt_bias.
+template <typename T, bool PACKED, bool GATE, bool FULL>
+__device__ __forceinline__ void grad_tile(const ScanParams& p, const ScanWork& w, int64_t tile, float* gs, float* as,
+                                          float* extra, float bias, float D, float& sumD, float& sumBias)
+{
+    const int lane = threadIdx.x, N = static_cast<int>(p.N);
+    const int64_t t0 = tile * kBwdTile, out = (w.row * p.T + t0) * p.E + w.e0;
+    const int64_t tiles = (p.T + kBwdTile - 1) / kBwdTile;
+    const int count = FULL ? kBwdTile : static_cast<int>(w.t1 - t0);
+    float d[kBwdTile], xv[kBwdTile], dyg[kBwdTile], du[kBwdTile], sa[kBwdTile], ys[kBwdTile];
+    // wanted again at the tile's end only, in shared memory meanwhile: the derivative of
+    // dt by dt_in, and dy silu'(z)
+    float* const slope = extra + lane;
+    float* const zd = slope + kBwdTile * 64;
+    unsigned starts = 0, ends = 0;   // bits (packed rows): the token starts / ends a sequence
     {
-        const int lane = threadIdx.x, N = static_cast<int>(p.N);
-        const int64_t t0 = tile * kBwdTile, out = (w.row * p.T + t0) * p.E + w.e0;
-        const int64_t tiles = (p.T + kBwdTile - 1) / kBwdTile;
-        const int count = FULL ? kBwdTile : static_cast<int>(w.t1 - t0);
-        float d[kBwdTile], slope[kBwdTile];   // dt and its derivative by dt_in
-        float xv[kBwdTile], dyg[kBwdTile], zd[kBwdTile], du[kBwdTile], sa[kBwdTile], ys[kBwdTile];
-        unsigned starts = 0, ends = 0;   // bits: the token starts / ends a sequence
-        {
-            Rows<const T> x(p.x, w.row * p.xb + t0 * p.xt + w.e0, p.xt);
-            Rows<const T> dt(p.dt, w.row * p.db + t0 * p.dtt + w.e0, p.dtt);
-            Rows<const T> z(GATE ? p.z : p.x, GATE ? w.row * p.zb + t0 * p.zt + w.e0 : 0, GATE ? p.zt : 0);
-            Rows<const T> dy(p.dy, out, p.E);
-            T xr[kBwdTile], dr[kBwdTile], yr[kBwdTile], zr[kBwdTile];
+        Rows<const T> x(p.x, w.row * p.xb + t0 * p.xt + w.e0, p.xt);
+        Rows<const T> dt(p.dt, w.row * p.db + t0 * p.dtt + w.e0, p.dtt);
+        Rows<const T> z(GATE ? p.z : p.x, GATE ? w.row * p.zb + t0 * p.zt + w.e0 : 0, GATE ? p.zt : 0);
+        Rows<const T> dy(p.dy, out, p.E);
+        T xr[kBwdTile], dr[kBwdTile], yr[kBwdTile], zr[kBwdTile];
 #pragma unroll
-            for (int u = 0; u < kBwdTile; ++u) {
-                xr[u] = x.get(w.lane);
-                dr[u] = dt.get(w.lane);
-                yr[u] = dy.get(w.lane);
-                if (GATE) zr[u] = z.get(w.lane);
-                const bool more = FULL || u + 1 < count;   // (at the end: the last token again)
-                if (u + 1 == kBwdTile) break;
-                x.move(more);
-                dt.move(more);
-                dy.move(more);
-                if (GATE) z.move(more);
-            }
+        for (int u = 0; u < kBwdTile; ++u) {
+            xr[u] = x.get(w.lane);
+            dr[u] = dt.get(w.lane);
+            yr[u] = dy.get(w.lane);
+            if (GATE) zr[u] = z.get(w.lane);
+            const bool more = FULL || u + 1 < count;   // (at the end: the last token again)
+            if (u + 1 == kBwdTile) break;
+            x.move(more);
+            dt.move(more);
+            dy.move(more);
+            if (GATE) z.move(more);
+        }
 #pragma unroll
-            for (int u = 0; u < kBwdTile; ++u) {
-                xv[u] = widen(xr[u]);
-                const float v = widen(dr[u]) + bias, dyv = w.live ? widen(yr[u]) : 0.f;
-                d[u] = v;
-                slope[u] = 1.f;
-                if (p.softplus) {
-                    const float e = exp_neg(fabsf(v));
-                    d[u] = softplus_hw(v, e);
-                    slope[u] = (v >= 0.f ? 1.f : e) * __builtin_amdgcn_rcpf(1.f + e);
-                }
-                dyg[u] = dyv;
-                if (GATE) {
-                    const float zv = widen(zr[u]), s = sigmoid_hw(zv);
-                    dyg[u] = dyv * zv * s;
-                    zd[u] = dyv * silu_grad(zv, s);
-                }
-                du[u] = sa[u] = ys[u] = 0.f;
-                if (PACKED && (FULL || u < count)) {
-                    if (scan_starts<PACKED>(p, t0 + u)) starts |= 1u << u;
-                    if (scan_ends<PACKED>(p, t0 + u)) ends |= 1u << u;
-                }
+        for (int u = 0; u < kBwdTile; ++u) {
+            xv[u] = widen(xr[u]);
+            const float v = widen(dr[u]) + bias, dyv = w.live ? widen(yr[u]) : 0.f;
+            d[u] = v;
+            if (p.softplus) {
+                const float e = exp_neg(fabsf(v));
+                d[u] = softplus_hw(v, e);
+                slope[u * 64] = (v >= 0.f ? 1.f : e) * __builtin_amdgcn_rcpf(1.f + e);
             }
-            if (!PACKED) {
-                starts = t0 == 0 ? 1u : 0u;
-                ends = t0 + count == p.T ? 1u << (count - 1) : 0u;
+            dyg[u] = dyv;
+            if (GATE) {
+                const float zv = widen(zr[u]), s = sigmoid_hw(zv);
+                dyg[u] = dyv * zv * s;
+                zd[u * 64] = dyv * silu_grad(zv, s);
+            }
+            du[u] = sa[u] = ys[u] = 0.f;
+            if (PACKED && (FULL || u < count)) {
+                if (scan_starts<PACKED>(p, t0 + u)) starts |= 1u << u;
+                if (scan_ends<PACKED>(p, t0 + u)) ends |= 1u << u;
             }
         }
-        Rows<const T> B0(p.B, w.row * p.bb + t0 * p.bt + w.g * p.N, p.bt), B1 = B0;
-        Rows<const T> C0(p.C, w.row * p.cb + t0 * p.ct + w.g * p.N, p.ct), C1 = C0;
-        const bool second = FULL || count > kHalf;   // there are tokens in the tile's second half
-        B1.p += second ? static_cast<int64_t>(kHalf) * p.bt : 0;
-        C1.p += second ? static_cast<int64_t>(kHalf) * p.ct : 0;
-        running(B1.p);
-        running(C1.p);
-        const int left0 = FULL ? kHalf : count, left1 = FULL ? kHalf : second ? count - kHalf : 1;
-        const float* m = p.marks + (w.row * tiles + tile) * p.N * p.E + w.e;
-        const float* A_log = p.A_log + w.e * p.N;
-        // the value that this lane gets of the 64: token, dB or dC, state
-        const int place = static_cast<int>(__brev(static_cast<unsigned>(lane)) >> 26);
-        const int tok = kBwdTile - 1 - place / (2 * kQuad);
-        float* to = p.pBC + (((w.tile * p.b + w.row) * p.T + t0 + tok) * p.G + w.g) * 2 * p.N +
-                    (place / kQuad % 2) * p.N + place % kQuad;
+    }
+    Rows<const T> B0(p.B, w.row * p.bb + t0 * p.bt + w.g * p.N, p.bt), B1 = B0;
+    Rows<const T> C0(p.C, w.row * p.cb + t0 * p.ct + w.g * p.N, p.ct), C1 = C0;
+    const bool second = FULL || count > kHalf;   // there are tokens in the tile's second half
+    B1.p += second ? static_cast<int64_t>(kHalf) * p.bt : 0;
+    C1.p += second ? static_cast<int64_t>(kHalf) * p.ct : 0;
+    running(B1.p);
+    running(C1.p);
+    const int left0 = FULL ? kHalf : count, left1 = FULL ? kHalf : second ? count - kHalf : 1;
+    Rows<const float> m(p.marks, (w.row * tiles + tile) * p.N * p.E + w.e0, p.E);
+    Rows<const float> entering(p.states, (w.row * p.S + w.chunk) * p.N * p.E + w.e0, p.E);
+    const float* A_log = p.A_log + w.e * p.N;
+    // whether the state entering the chunk reaches the tile (no sequence starts in between)
+    bool reached = w.chunk > 0;
+    if (PACKED && reached)
+        reached = !scan_starts<PACKED>(p, w.t0) &&
+                  scalar_load(p.seq_idx + w.t0) == scalar_load(p.seq_idx + (t0 > w.t0 ? t0 - 1 : t0));
+    const float since = p.marksums[(w.row * tiles + tile) * p.E + w.e];
+    // the value that this lane gets of the 64: token, dB or dC, state
+    const int place = static_cast<int>(__brev(static_cast<unsigned>(lane)) >> 26);
+    const int tok = kBwdTile - 1 - place / (2 * kQuad);
+    float* to = p.pBC + (((w.tile * p.b + w.row) * p.T + t0 + tok) * p.G + w.g) * 2 * p.N +
+                (place / kQuad % 2) * p.N + place % kQuad;
 
-        for (int q = 0; q < N; q += kQuad) {
-            float A2[kQuad], h[kQuad], g[kQuad], dA[kQuad];
-            float hb[kBwdTile][kQuad], a[kBwdTile][kQuad];   // state before each token, its decay
-            QuadRows<T> lo, hi;
-            lo.load(B0, C0, left0);
+    // a round's own values, loaded a round ahead
+    float4 al;
+    float mn[kQuad], en[kQuad] = {};
+    const auto ahead = [&](int q) {
+        al = *reinterpret_cast<const float4*>(A_log + q);
+#pragma unroll
+        for (int n = 0; n < kQuad; ++n) {
+            mn[n] = m.get(w.lane);
+            m.move();
+        }
+        if (reached) {
 #pragma unroll
             for (int n = 0; n < kQuad; ++n) {
-                A2[n] = decay_rate(A_log[q + n]);
-                h[n] = m[n * p.E];
-                g[n] = gs[(q + n) * 64];
-                dA[n] = as[(q + n) * 64];
+                en[n] = entering.get(w.lane);
+                entering.move();
             }
-            lo.arrive();
-            hi.load(B1, C1, left1);
-            __builtin_amdgcn_sched_barrier(0);
-            each<0, kBwdTile>([&](auto i) {
-                constexpr int u = decltype(i)::value, k = u % kHalf;
-                if constexpr (u == kHalf) hi.arrive();
-                if (!FULL && u >= count) return;
-                if (PACKED && (starts >> u & 1)) {
-                    const int64_t unit = scan_unit<PACKED>(p, w.row, t0 + u);
+        }
+    };
+    ahead(0);
+    for (int q = 0; q < N; q += kQuad) {
+        float A2[kQuad], h[kQuad], g[kQuad], dA[kQuad];
+        float hb[kBwdTile][kQuad], a[kBwdTile][kQuad];   // state before each token, its decay
+        QuadRows<T> lo, hi;
+        lo.load(B0, C0, left0);
+        A2[0] = decay_rate(al.x);
+        A2[1] = decay_rate(al.y);
+        A2[2] = decay_rate(al.z);
+        A2[3] = decay_rate(al.w);
 #pragma unroll
-                    for (int n = 0; n < kQuad; ++n) h[n] = p.init ? p.init[(unit * p.E + w.e) * p.N + q + n] : 0.f;
-                }
-                const QuadRows<T>& bc = u < kHalf ? lo : hi;
+        for (int n = 0; n < kQuad; ++n) {
+            // (nothing reaches the tile: 0 times a decay)
+            h[n] = fmaf(__builtin_amdgcn_exp2f(since * A2[n]), en[n], mn[n]);
+            g[n] = gs[(q + n) * 64];
+            dA[n] = as[(q + n) * 64];
+        }
+        if (q + kQuad < N) ahead(q + kQuad);
+        lo.arrive();
+        hi.load(B1, C1, left1);
+        __builtin_amdgcn_sched_barrier(0);
+        each<0, kBwdTile>([&](auto i) {
+            constexpr int u = decltype(i)::value, k = u % kHalf;
+            if constexpr (u == kHalf) hi.arrive();
+            if (!FULL && u >= count) return;
+            if (PACKED && (starts >> u & 1)) {
+                const int64_t unit = scan_unit<PACKED>(p, w.row, t0 + u);
+#pragma unroll
+                for (int n = 0; n < kQuad; ++n) h[n] = p.init ? p.init[(unit * p.E + w.e) * p.N + q + n] : 0.f;
+            }
+            const Uniform<T, kQuad>&b = half<(u < kHalf)>(lo, hi).b[k], &c = half<(u < kHalf)>(lo, hi).c[k];
+            const float in = d[u] * xv[u];
+#pragma unroll
+            for (int n = 0; n < kQuad; ++n) {
+                a[u][n] = __builtin_amdgcn_exp2f(d[u] * A2[n]);
+                hb[u][n] = h[n];
+                h[n] = fmaf(a[u][n], h[n], in * b[n]);
+                if (GATE) ys[u] = fmaf(h[n], c[n], ys[u]);
+            }
+        });
+        // a sequence's last token: g is the final state's gradient; its first one: g is
+        // the initial state's
+        const auto leave = [&](int u) {
+            const int64_t unit = scan_unit<PACKED>(p, w.row, t0 + u);
+#pragma unroll
+            for (int n = 0; n < kQuad; ++n)
+                g[n] = p.dfin && w.live ? p.dfin[(unit * p.E + w.e) * p.N + q + n] : 0.f;
+        };
+        const auto arrive = [&](int u) {
+            if (!p.dinit || !w.live) return;
+            const int64_t unit = scan_unit<PACKED>(p, w.row, t0 + u);
+#pragma unroll
+            for (int n = 0; n < kQuad; ++n) p.dinit[(unit * p.E + w.e) * p.N + q + n] = g[n];
+        };
+        if (!PACKED && t0 + count == p.T) leave(count - 1);
+        LaneSums sums;
+        lo.load(B0, C0, left0);   // (again, for the way back)
+        __builtin_amdgcn_sched_barrier(0);
+        each<0, kBwdTile>([&](auto i) {
+            constexpr int I = decltype(i)::value, u = kBwdTile - 1 - I;
+            constexpr int first = I * 2 * kQuad, k = u % kHalf;
+            if constexpr (u == kHalf - 1) lo.arrive();
+            // the token's products for dB and dC (one place of the tree each; a token past
+            // the end puts zeros)
+            float products[2 * kQuad] = {};
+            if (FULL || u < count) {
+                const Uniform<T, kQuad>&b = half<(u < kHalf)>(lo, hi).b[k], &c = half<(u < kHalf)>(lo, hi).c[k];
                 const float in = d[u] * xv[u];
+                if (PACKED && (ends >> u & 1)) leave(u);
 #pragma unroll
                 for (int n = 0; n < kQuad; ++n) {
-                    a[u][n] = __builtin_amdgcn_exp2f(d[u] * A2[n]);
-                    hb[u][n] = h[n];
-                    h[n] = fmaf(a[u][n], h[n], in * bc.b[k][n]);
-                    if (GATE) ys[u] = fmaf(h[n], bc.c[k][n], ys[u]);
-                }
-            });
-            lo.load(B0, C0, left0);   // (again, for the way back)
-            __builtin_amdgcn_sched_barrier(0);
-            LaneSums sums;
-            each<0, kBwdTile>([&](auto i) {
-                constexpr int I = decltype(i)::value, u = kBwdTile - 1 - I, k = u % kHalf;
-                constexpr int first = I * 2 * kQuad;
-                if constexpr (u == kHalf - 1) lo.arrive();
-                if (!FULL && u >= count) {
-                    each<0, 2 * kQuad>([&](auto n) { sums.template put<first + decltype(n)::value>(0.f, lane); });
-                    return;
-                }
-                const QuadRows<T>& bc = u < kHalf ? lo : hi;
-                const float in = d[u] * xv[u];
-                if (ends >> u & 1) {
-                    const int64_t unit = scan_unit<PACKED>(p, w.row, t0 + u);
-#pragma unroll
-                    for (int n = 0; n < kQuad; ++n)
-                        g[n] = p.dfin && w.live ? p.dfin[(unit * p.E + w.e) * p.N + q + n] : 0.f;
-                }
-#pragma unroll
-                for (int n = 0; n < kQuad; ++n) {
-                    g[n] = fmaf(dyg[u], bc.c[k][n], g[n]);
-                    du[u] = fmaf(g[n], bc.b[k][n], du[u]);
-                }
-                each<0, kQuad>([&](auto n) { sums.template put<first + decltype(n)::value>(g[n] * in, lane); });
-                each<0, kQuad>([&](auto j) {
-                    constexpr int n = decltype(j)::value;
+                    g[n] = fmaf(dyg[u], c[n], g[n]);
+                    du[u] = fmaf(g[n], b[n], du[u]);
+                    products[n] = g[n] * in;
                     // the state after the token: that before the next one, if no sequence starts there
                     float after;
                     if constexpr (PACKED || !FULL)
-                        after = fmaf(a[u][n], hb[u][n], in * bc.b[k][n]);
+                        after = fmaf(a[u][n], hb[u][n], in * b[n]);
                     else
                         after = u + 1 < kBwdTile ? hb[u + 1 < kBwdTile ? u + 1 : u][n] : h[n];
-                    sums.template put<first + kQuad + n>(dyg[u] * after, lane);
-                });
-#pragma unroll
-                for (int n = 0; n < kQuad; ++n) {
+                    products[kQuad + n] = dyg[u] * after;
                     g[n] *= a[u][n];
                     const float e = g[n] * hb[u][n];
                     sa[u] = fmaf(e, A2[n], sa[u]);
                     dA[n] = fmaf(e, d[u], dA[n]);
                 }
-                if ((PACKED || u == 0) && (starts >> u & 1) && p.dinit && w.live) {
-                    const int64_t unit = scan_unit<PACKED>(p, w.row, t0 + u);
-#pragma unroll
-                    for (int n = 0; n < kQuad; ++n) p.dinit[(unit * p.E + w.e) * p.N + q + n] = g[n];
-                }
+                if (PACKED && (starts >> u & 1)) arrive(u);
+            }
+            each<0, 2 * kQuad>([&](auto n) {
+                sums.template put<first + decltype(n)::value>(products[decltype(n)::value], lane);
             });
-            if (FULL || tok < count) *to = sums.out;
+        });
+        if (!PACKED && t0 == 0) arrive(0);
+        if (FULL || tok < count) *to = sums.out;
 #pragma unroll
-            for (int n = 0; n < kQuad; ++n) {
-                gs[(q + n) * 64] = g[n];
-                as[(q + n) * 64] = dA[n];
-            }
-            B0.p += kQuad;
-            C0.p += kQuad;
-            B1.p += kQuad;
-            C1.p += kQuad;
-            m += kQuad * p.E;
-            to += kQuad;
+        for (int n = 0; n < kQuad; ++n) {
+            gs[(q + n) * 64] = g[n];
+            as[(q + n) * 64] = dA[n];
         }
+        to += kQuad;
+        B0.p += kQuad;
+        C0.p += kQuad;
+        B1.p += kQuad;
+        C1.p += kQuad;
+    }
 
-        Rows<T> dx(p.dx, out, p.E), ddt(p.ddt, out, p.E), dz(GATE ? p.dz : p.dx, out, p.E);
+    Rows<T> dx(p.dx, out, p.E), ddt(p.ddt, out, p.E), dz(GATE ? p.dz : p.dx, out, p.E);
 #pragma unroll
-        for (int u = 0; u < kBwdTile; ++u) {
-            if (FULL || u < count) {
-                const float dd = fmaf(xv[u], du[u], sa[u] * 0.69314718f) * slope[u];   // (A2 is A log2(e))
-                sumD = fmaf(dyg[u], xv[u], sumD);
-                sumBias += dd;
-                if (w.live) {
-                    dx.put(w.lane, narrow<T>(fmaf(d[u], du[u], D * dyg[u])));
-                    ddt.put(w.lane, narrow<T>(dd));
-                    if (GATE) dz.put(w.lane, narrow<T>(zd[u] * fmaf(D, xv[u], ys[u])));
-                }
-                dx.move();
-                ddt.move();
-                if (GATE) dz.move();
+    for (int u = 0; u < kBwdTile; ++u) {
+        if (FULL || u < count) {
+            float dd = fmaf(xv[u], du[u], sa[u] * 0.69314718f);   // (A2 is A log2(e))
+            if (p.softplus) dd *= slope[u * 64];
+            sumD = fmaf(dyg[u], xv[u], sumD);
+            sumBias += dd;
+            if (w.live) {
+                dx.put(w.lane, narrow<T>(fmaf(d[u], du[u], D * dyg[u])));
+                ddt.put(w.lane, narrow<T>(dd));
+                if (GATE) dz.put(w.lane, narrow<T>(zd[u * 64] * fmaf(D, xv[u], ys[u])));
             }
+            dx.move();
+            ddt.move();
+            if (GATE) dz.move();
         }
     }
-};
+}
 
+// One wavefront: 64 channels of one chunk, its tiles from the last to the first.
+// Shared memory: the states' running gradients g and sums of dA, [2][N][64], and two
+// values of each of the tile's tokens, [2][kBwdTile][64].
 template <typename T, bool PACKED, bool GATE>
 __global__ __launch_bounds__(64, 2) void k_scan_grad(ScanParams p)
 {
     extern __shared__ float shared[];
     const int lane = threadIdx.x, N = static_cast<int>(p.N);
     const ScanWork w = scan_work(p, blockIdx.x);
-    GradTile<T, PACKED, GATE> g{p, w, shared + lane, shared + N * 64 + lane,
-                                p.dt_bias ? p.dt_bias[w.e] : 0.f, p.D ? p.D[w.e] : 0.f, 0.f, 0.f};
+    float* const gs = shared + lane;
+    float* const as = shared + N * 64 + lane;
+    float* const extra = shared + 2 * N * 64;
+    const float bias = p.dt_bias ? p.dt_bias[w.e] : 0.f, D = p.D ? p.D[w.e] : 0.f;
+    float sumD = 0.f, sumBias = 0.f;
     const float* from = p.rstates + (w.row * p.S + w.chunk) * p.N * p.E + w.e;
     for (int n = 0; n < N; ++n) {
-        g.gs[n * 64] = w.live && p.S > 1 ? from[n * p.E] : 0.f;
-        g.as[n * 64] = 0.f;
+        gs[n * 64] = w.live && p.S > 1 ? from[n * p.E] : 0.f;
+        as[n * 64] = 0.f;
     }
     int64_t tile = (w.t1 - 1) / kBwdTile;
-    if (w.t1 - tile * kBwdTile < kBwdTile) g.template run<false>(tile--);
-    for (; tile * kBwdTile >= w.t0; --tile) g.template run<true>(tile);
+    if (w.t1 - tile * kBwdTile < kBwdTile) {
+        grad_tile<T, PACKED, GATE, false>(p, w, tile, gs, as, extra, bias, D, sumD, sumBias);
+        --tile;
+    }
+    for (; tile * kBwdTile >= w.t0; --tile)
+        grad_tile<T, PACKED, GATE, true>(p, w, tile, gs, as, extra, bias, D, sumD, sumBias);
     if (!w.live) return;
     const int64_t rc = w.row * p.S + w.chunk;
-    for (int n = 0; n < N; ++n) p.pA[(rc * p.N + n) * p.E + w.e] = g.as[n * 64];
-    p.pD[rc * 2 * p.E + w.e] = g.sumD;
-    p.pD[(rc * 2 + 1) * p.E + w.e] = g.sumBias;
+    for (int n = 0; n < N; ++n) p.pA[(rc * p.N + n) * p.E + w.e] = as[n * 64];
+    p.pD[rc * 2 * p.E + w.e] = sumD;
+    p.pD[(rc * 2 + 1) * p.E + w.e] = sumBias;
 }
 
-// dA_log, dD and ddt_bias: sums over rows and chunks, eight interleaved ones a
+// dA_log, dD and ddt_bias: sums over rows and chunks, 32 interleaved ones a
 // column joined at the end.
-constexpr int kSumLanes = 8, kSumCols = 32;
+constexpr int kSumLanes = 32, kSumCols = 32;
 
 __global__ __launch_bounds__(kSumLanes * kSumCols) void k_scan_sum_params(ScanParams p)
 {
@@ -419,8 +466,8 @@ __global__ __launch_bounds__(256) void k_scan_sum_bc(ScanParams p, int64_t block
 template <typename T, bool PACKED, bool GATE>
 hipError_t grad(const ScanParams& p, int64_t units, hipStream_t stream)
 {
-    const size_t lds = 2 * static_cast<size_t>(p.N) * 64 * sizeof(float);
-    if (lds > 65536) {   // (N > 128) beyond the default limit
+    const size_t lds = 2 * static_cast<size_t>(p.N + kBwdTile) * 64 * sizeof(float);
+    if (lds > 65536) {   // (N > 120) beyond the default limit
         const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_scan_grad<T, PACKED, GATE>),
                                                    hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));
         if (err != hipSuccess) return err;
@@ -436,12 +483,11 @@ hipError_t run(const ScanParams& p, hipStream_t stream)
     const int64_t sums = (p.N * p.E + 2 * p.E + kSumCols - 1) / kSumCols, bc = (p.b * p.T * p.G * 2 * p.N + 255) / 256;
     const int64_t pass = (p.b * p.N * p.E + 255) / 256;
     if (units > kMaxGrid || sums > kMaxGrid || bc > kMaxGrid || pass > kMaxGrid) return hipErrorInvalidConfiguration;
+    if (hipError_t err = launch_scan_both(p, sizeof(T) == 2, stream); err != hipSuccess) return err;
     if (p.S > 1) {
-        if (hipError_t err = launch_scan_chunk_states(p, sizeof(T) == 2, false, stream); err != hipSuccess) return err;
         if (hipError_t err = launch_scan_pass(p, stream); err != hipSuccess) return err;
         hipLaunchKernelGGL(k_scan_rev_pass, dim3(static_cast<unsigned>(pass)), dim3(256), 0, stream, p);
     }
-    if (hipError_t err = launch_scan_chunk_states(p, sizeof(T) == 2, true, stream); err != hipSuccess) return err;
     if (hipError_t err = p.z ? grad<T, PACKED, true>(p, units, stream) : grad<T, PACKED, false>(p, units, stream);
         err != hipSuccess)
         return err;
