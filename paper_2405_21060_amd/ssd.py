@@ -18,7 +18,6 @@ convolution), :func:`scan_forward`, :func:`scan_backward`, :func:`scan_step`
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import os
 from typing import Optional, Tuple
@@ -816,14 +815,18 @@ def forward_varlen(x, dt, A_log, B, C, seq_starts, D=None, chunk_size: int = 256
 
 # ---- What stands around the layer in a block -------------------------------------------
 
-_NO_GUARD = contextlib.nullcontext()
-
-
-def _device(index: int):
-    """Makes a device current for a call's launches, where it is not already."""
+def _launch(index: int, name: str, *args) -> None:
+    """A call of the library on torch's current stream of a device, which is made
+    current for it where it is not."""
     import torch
 
-    return _NO_GUARD if torch._C._cuda_getDevice() == index else torch.cuda.device(index)
+    if torch._C._cuda_getDevice() == index:
+        rc = getattr(_lib or load_library(), name)(*args, torch._C._cuda_getCurrentRawStream(index))
+    else:
+        with torch.cuda.device(index):
+            rc = getattr(_lib or load_library(), name)(*args, torch._C._cuda_getCurrentRawStream(index))
+    if rc != SSD_OK:
+        raise SsdError(rc, name)
 
 
 def _act_dtype(x) -> int:
@@ -910,17 +913,6 @@ def _sized(name, prob):
     return int(need.value)
 
 
-def _done(rc: int, where: str) -> None:
-    if rc != SSD_OK:
-        raise SsdError(rc, where)
-
-
-def _stream(index: int) -> int:
-    import torch
-
-    return torch._C._cuda_getCurrentRawStream(index)
-
-
 def _conv_problem(x, weight, split, silu, nseq, dtype):
     b, T, C = x.shape
     split = (C,) if split is None else tuple(int(k) for k in split)
@@ -963,11 +955,8 @@ def conv_forward(x, weight, bias=None, silu: bool = True, initial_states=None, s
         raise ValueError("out must have as many parts as split")
     ys = tuple(_out(o, (b, T, k), x.dtype, x.device) for o, k in zip(outs, sizes))
     fin = _out(None, (units, W - 1, C), x.dtype, x.device) if return_final_states else None
-    on = x.get_device()
-    with _device(on):
-        _done(load_library().ssd_conv_forward(ctypes.byref(prob), _ptr(x), _ptr(weight), _ptr(bias),
-                                              _ptr(initial_states), _ptr(seq_idx), _pointers(ys), _ptr(fin),
-                                              _stream(on)), "ssd_conv_forward")
+    _launch(x.get_device(), "ssd_conv_forward", prob, _ptr(x), _ptr(weight), _ptr(bias), _ptr(initial_states),
+            _ptr(seq_idx), _pointers(ys), _ptr(fin))
     return (ys[0] if split is None else ys), fin
 
 
@@ -996,32 +985,47 @@ def conv_backward(x, weight, dy, bias=None, silu: bool = True, initial_states=No
     g = {"dx": torch.empty((b, T, C), dtype=x.dtype, device=x.device), "dweight": torch.empty_like(weight),
          "dbias": torch.empty_like(bias) if bias is not None else None,
          "dinit": torch.empty(state, dtype=x.dtype, device=x.device)}
-    on = x.get_device()
-    with _device(on):
-        _done(load_library().ssd_conv_backward(
-            ctypes.byref(prob), _ptr(x), _ptr(weight), _ptr(bias), _ptr(initial_states), _ptr(seq_idx), _pointers(dys),
-            _ptr(dfinal_states), _ptr(g["dx"]), _ptr(g["dweight"]), _ptr(g["dbias"]), _ptr(g["dinit"]),
-            _ptr(workspace), need, _stream(on)), "ssd_conv_backward")
+    _launch(x.get_device(), "ssd_conv_backward", prob, _ptr(x), _ptr(weight), _ptr(bias), _ptr(initial_states),
+            _ptr(seq_idx), _pointers(dys), _ptr(dfinal_states), _ptr(g["dx"]), _ptr(g["dweight"]), _ptr(g["dbias"]),
+            _ptr(g["dinit"]), _ptr(workspace), need)
     return g
 
 
 def conv_step(x, weight, state, bias=None, silu: bool = True, out=None):
     """One token of ``conv_forward`` per row: x (b,C) (rows may be strided), state
     (b,W-1,C) in x's dtype, moved on in place; returns y (b,C)."""
-    dtype = _act_dtype(x)
+    import torch
+
+    # One expression over what the checks ask for (the call is shorter on the device
+    # than its checks are here); they say what is wrong when it fails.
+    f32, t, on = torch.float32, x.dtype, x.get_device()
+    if not (x.is_cuda and (t is torch.bfloat16 or t is f32) and x.dim() == 2 and weight.dim() == 2
+            and state.dtype is t and weight.dtype is f32 and state.get_device() == on and weight.get_device() == on
+            and x.stride(1) == 1 and state.is_contiguous() and weight.is_contiguous()
+            and state.shape == (x.shape[0], weight.shape[1] - 1, x.shape[1]) and weight.shape[0] == x.shape[1]
+            and (bias is None or (bias.dtype is f32 and bias.get_device() == on and bias.is_contiguous()
+                                  and bias.shape == (x.shape[1],)))):
+        _check_conv_step(x, weight, state, bias)
+    b, C = x.shape
+    y = torch.empty((b, C), dtype=t, device=x.device) if out is None else _out(out, (b, C), t, x.device)
+    prob = SsdConvProblem(b, 1, C, weight.shape[1], 0, x.stride(0), 0, 1, _NO_PARTS,
+                          SSD_DTYPE_F32 if t is f32 else SSD_DTYPE_BF16, 1 if silu else 0)
+    _launch(on, "ssd_conv_step", prob, x.data_ptr(), weight.data_ptr(), _ptr(bias), state.data_ptr(), y.data_ptr())
+    return y
+
+
+_NO_PARTS = (ctypes.c_int64 * 3)()
+
+
+def _check_conv_step(x, weight, state, bias):
+    """The checks of ``conv_step``, one by one."""
+    _act_dtype(x)
     if x.dim() != 2 or weight.dim() != 2:
         raise ValueError("x and weight must have 2 dimensions")
     b, C = x.shape
     W = weight.shape[1]
     _check(x, act=(("state", state, (b, W - 1, C)),), f32=(("weight", weight, (C, W)), ("bias", bias, (C,))),
            strided=(("x", x, (b, C)),))
-    y = _out(out, (b, C), x.dtype, x.device)
-    prob = SsdConvProblem(b, 1, C, W, 0, x.stride(0), 0, 1, (ctypes.c_int64 * 3)(C, 0, 0), dtype, int(bool(silu)))
-    on = x.get_device()
-    with _device(on):
-        _done(load_library().ssd_conv_step(ctypes.byref(prob), _ptr(x), _ptr(weight), _ptr(bias), _ptr(state), _ptr(y),
-                                           _stream(on)), "ssd_conv_step")
-    return y
 
 
 def _scan_problem(x, dt, B, C, z, softplus, nseq, dtype):
@@ -1077,12 +1081,8 @@ def scan_forward(x, dt, A_log, B, C, D=None, z=None, dt_bias=None, dt_softplus: 
     fin = None
     if return_final_states:
         fin = _out(final_out, (units, E, B.shape[3]), torch.float32, x.device, "final_out")
-    on = x.get_device()
-    with _device(on):
-        _done(load_library().ssd_scan_forward(
-            ctypes.byref(prob), _ptr(x), _ptr(dt), _ptr(A_log), _ptr(B), _ptr(C), _ptr(D), _ptr(z), _ptr(dt_bias),
-            _ptr(initial_states), _ptr(seq_idx), _ptr(y), _ptr(fin), _ptr(workspace), need, _stream(on)),
-            "ssd_scan_forward")
+    _launch(x.get_device(), "ssd_scan_forward", prob, _ptr(x), _ptr(dt), _ptr(A_log), _ptr(B), _ptr(C), _ptr(D),
+            _ptr(z), _ptr(dt_bias), _ptr(initial_states), _ptr(seq_idx), _ptr(y), _ptr(fin), _ptr(workspace), need)
     return y, fin
 
 
@@ -1105,20 +1105,48 @@ def scan_backward(x, dt, A_log, B, C, dy, D=None, z=None, dt_bias=None, dt_softp
     g = {"dx": new(x), "ddt": new(x), "dB": new(B), "dC": new(C), "dz": new(z), "dA_log": new(A_log), "dD": new(D),
          "ddt_bias": new(dt_bias),
          "dinit": torch.empty((units, x.shape[2], B.shape[3]), dtype=torch.float32, device=x.device)}
-    on = x.get_device()
-    with _device(on):
-        _done(load_library().ssd_scan_backward(
-            ctypes.byref(prob), _ptr(x), _ptr(dt), _ptr(A_log), _ptr(B), _ptr(C), _ptr(D), _ptr(z), _ptr(dt_bias),
-            _ptr(initial_states), _ptr(seq_idx), _ptr(dy), _ptr(dfinal_states), _ptr(g["dx"]), _ptr(g["ddt"]),
-            _ptr(g["dA_log"]), _ptr(g["dB"]), _ptr(g["dC"]), _ptr(g["dD"]), _ptr(g["dz"]), _ptr(g["ddt_bias"]),
-            _ptr(g["dinit"]), _ptr(workspace), need, _stream(on)), "ssd_scan_backward")
+    _launch(x.get_device(), "ssd_scan_backward", prob, _ptr(x), _ptr(dt), _ptr(A_log), _ptr(B), _ptr(C), _ptr(D),
+            _ptr(z), _ptr(dt_bias), _ptr(initial_states), _ptr(seq_idx), _ptr(dy), _ptr(dfinal_states), _ptr(g["dx"]),
+            _ptr(g["ddt"]), _ptr(g["dA_log"]), _ptr(g["dB"]), _ptr(g["dC"]), _ptr(g["dD"]), _ptr(g["dz"]),
+            _ptr(g["ddt_bias"]), _ptr(g["dinit"]), _ptr(workspace), need)
     return g
 
 
 def scan_step(x, dt, A_log, B, C, state, D=None, z=None, dt_bias=None, dt_softplus: bool = True, out=None):
     """One token of ``scan_forward`` per row: x, dt, z (b,E), B, C (b,G,N) (rows may be
     strided), state (b,E,N) float32, updated in place; returns y (b,E)."""
-    dtype = _act_dtype(x)
+    import torch
+
+    # (as in conv_step: one expression, and the checks one by one where it fails)
+    f32, t, on = torch.float32, x.dtype, x.get_device()
+    if not (x.is_cuda and (t is torch.bfloat16 or t is f32) and x.dim() == 2 and B.dim() == 3
+            and dt.dtype is t and B.dtype is t and C.dtype is t and A_log.dtype is f32 and state.dtype is f32
+            and dt.get_device() == on and B.get_device() == on and C.get_device() == on
+            and A_log.get_device() == on and state.get_device() == on
+            and A_log.is_contiguous() and state.is_contiguous() and x.stride(1) == 1 and dt.stride(1) == 1
+            and B.stride(2) == 1 and C.stride(2) == 1 and B.stride(1) == B.shape[2] and C.stride(1) == B.shape[2]
+            and dt.shape == x.shape and B.shape[0] == x.shape[0] and C.shape == B.shape
+            and A_log.shape == (x.shape[1], B.shape[2]) and state.shape == (x.shape[0], x.shape[1], B.shape[2])
+            and (z is None or (z.dtype is t and z.get_device() == on and z.shape == x.shape and z.stride(1) == 1))
+            and (D is None or (D.dtype is f32 and D.get_device() == on and D.is_contiguous()
+                               and D.shape == (x.shape[1],)))
+            and (dt_bias is None or (dt_bias.dtype is f32 and dt_bias.get_device() == on and dt_bias.is_contiguous()
+                                     and dt_bias.shape == (x.shape[1],)))):
+        _check_scan_step(x, dt, A_log, B, C, state, D, z, dt_bias)
+    b, E = x.shape
+    G, N = B.shape[1:]
+    y = torch.empty((b, E), dtype=t, device=x.device) if out is None else _out(out, (b, E), t, x.device)
+    prob = SsdScanProblem(b, 1, E, N, G, 0, x.stride(0), 0, dt.stride(0), 0, z.stride(0) if z is not None else 0, 0,
+                          B.stride(0), 0, C.stride(0), 0, SSD_DTYPE_F32 if t is f32 else SSD_DTYPE_BF16,
+                          1 if dt_softplus else 0)
+    _launch(on, "ssd_scan_step", prob, x.data_ptr(), dt.data_ptr(), A_log.data_ptr(), B.data_ptr(), C.data_ptr(),
+            _ptr(D), _ptr(z), _ptr(dt_bias), state.data_ptr(), y.data_ptr())
+    return y
+
+
+def _check_scan_step(x, dt, A_log, B, C, state, D, z, dt_bias):
+    """The checks of ``scan_step``, one by one."""
+    _act_dtype(x)
     if x.dim() != 2 or B.dim() != 3:
         raise ValueError("x must have 2 dimensions and B and C 3")
     b, E = x.shape
@@ -1128,15 +1156,6 @@ def scan_step(x, dt, A_log, B, C, state, D=None, z=None, dt_bias=None, dt_softpl
             raise ValueError("%s's groups must be contiguous" % name)
     _check(x, f32=(("A_log", A_log, (E, N)), ("D", D, (E,)), ("dt_bias", dt_bias, (E,)), ("state", state, (b, E, N))),
            strided=(("x", x, (b, E)), ("dt", dt, (b, E)), ("z", z, (b, E)), ("B", B, (b, G, N)), ("C", C, (b, G, N))))
-    y = _out(out, (b, E), x.dtype, x.device)
-    prob = SsdScanProblem(b, 1, E, N, G, 0, x.stride(0), 0, dt.stride(0), 0, z.stride(0) if z is not None else 0, 0,
-                          B.stride(0), 0, C.stride(0), 0, dtype, int(bool(dt_softplus)))
-    on = x.get_device()
-    with _device(on):
-        _done(load_library().ssd_scan_step(ctypes.byref(prob), _ptr(x), _ptr(dt), _ptr(A_log), _ptr(B), _ptr(C),
-                                           _ptr(D), _ptr(z), _ptr(dt_bias), _ptr(state), _ptr(y), _stream(on)),
-              "ssd_scan_step")
-    return y
 
 
 def _norm_checked(x, weight, residual, residual_dtype, act=(), whole=()):
@@ -1157,20 +1176,28 @@ def _norm_checked(x, weight, residual, residual_dtype, act=(), whole=()):
     return dtype, SSD_DTYPE_F32 if kind == torch.float32 else SSD_DTYPE_BF16, kind, x.numel() // C if C else 0, C
 
 
-def _add_norm(x, weight, residual, eps, residual_dtype, out_type, out_dtype, scaled):
+def _add_norm(x, weight, residual, eps, residual_dtype, out_type, out_dtype):
     import torch
 
-    dtype, res, kind, rows, C = _norm_checked(x, weight, residual, residual_dtype)
+    # (as in conv_step: one expression, and the checks one by one where it fails)
+    f32, t, on = torch.float32, x.dtype, x.get_device()
+    if (x.is_cuda and (t is torch.bfloat16 or t is f32) and x.dim() >= 1 and x.numel() > 0 and x.is_contiguous()
+            and residual is not None and residual_dtype is None and (residual.dtype is t or residual.dtype is f32)
+            and residual.get_device() == on and residual.is_contiguous() and residual.shape == x.shape
+            and (weight is None or (weight.dtype is f32 and weight.get_device() == on and weight.is_contiguous()
+                                    and weight.shape == (x.shape[-1],)))):
+        dtype, kind, C = SSD_DTYPE_F32 if t is f32 else SSD_DTYPE_BF16, residual.dtype, x.shape[-1]
+        res, rows = SSD_DTYPE_F32 if kind is f32 else SSD_DTYPE_BF16, x.numel() // C
+    else:
+        dtype, res, kind, rows, C = _norm_checked(x, weight, residual, residual_dtype)
     # without a residual and in x's own dtype, r is x
-    keep = residual is not None or kind != x.dtype
-    r = torch.empty(x.shape, dtype=kind, device=x.device) if keep else x
-    y = torch.empty(x.shape, dtype=out_type or x.dtype, device=x.device)
-    scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if scaled else None
-    prob = SsdNormProblem(rows, C, dtype, res, dtype if out_dtype is None else out_dtype, float(eps))
-    on = x.get_device()
-    with _device(on):
-        _done(load_library().ssd_add_norm(ctypes.byref(prob), _ptr(x), _ptr(residual), _ptr(weight), _ptr(y),
-                                          _ptr(scale), _ptr(r) if keep else None, _stream(on)), "ssd_add_norm")
+    keep = residual is not None or kind != t
+    r = x if not keep else torch.empty_like(x) if kind is t else torch.empty_like(x, dtype=kind)
+    y = torch.empty_like(x) if out_type is None else torch.empty_like(x, dtype=out_type)
+    scale = torch.empty(x.shape[:-1], dtype=f32, device=x.device) if out_type is not None else None
+    prob = SsdNormProblem(rows, C, dtype, res, dtype if out_dtype is None else out_dtype, eps)
+    _launch(on, "ssd_add_norm", prob, x.data_ptr(), _ptr(residual), _ptr(weight), y.data_ptr(), _ptr(scale),
+            r.data_ptr() if keep else None)
     return y, scale, r
 
 
@@ -1180,7 +1207,7 @@ def add_norm(x, weight=None, residual=None, eps: float = 1e-5, residual_dtype=No
     is no residual yet) and y = r / sqrt(mean(r^2) + eps) * weight in x's dtype, over
     the last dimension.  Without a residual and in x's dtype r is x itself.  x and
     residual are contiguous, weight (C,) float32."""
-    y, _, r = _add_norm(x, weight, residual, eps, residual_dtype, None, None, False)
+    y, _, r = _add_norm(x, weight, residual, eps, residual_dtype, None, None)
     return y, r
 
 
@@ -1191,11 +1218,11 @@ def add_norm_q8(x, weight=None, residual=None, eps: float = 1e-5, residual_dtype
     type's range).  A row with a NaN or an infinity has scale NaN."""
     import torch
 
-    kinds = {torch.int8: SSD_DTYPE_I8, torch.float8_e4m3fn: SSD_DTYPE_E4M3}
-    dtype = torch.float8_e4m3fn if dtype is None else dtype
-    if dtype not in kinds:
+    if dtype is None or dtype is torch.float8_e4m3fn:
+        return _add_norm(x, weight, residual, eps, residual_dtype, torch.float8_e4m3fn, SSD_DTYPE_E4M3)
+    if dtype is not torch.int8:
         raise TypeError("dtype must be torch.int8 or torch.float8_e4m3fn")
-    return _add_norm(x, weight, residual, eps, residual_dtype, dtype, kinds[dtype], True)
+    return _add_norm(x, weight, residual, eps, residual_dtype, dtype, SSD_DTYPE_I8)
 
 
 def add_norm_backward(dy, residual, weight=None, dresidual=None, eps: float = 1e-5, workspace=None):
@@ -1214,10 +1241,6 @@ def add_norm_backward(dy, residual, weight=None, dresidual=None, eps: float = 1e
     dx = torch.empty_like(dy)
     dr = dx if kind == dy.dtype else torch.empty(dy.shape, dtype=kind, device=dy.device)
     g = {"dx": dx, "dresidual": dr, "dweight": torch.empty_like(weight) if weight is not None else None}
-    on = dy.get_device()
-    with _device(on):
-        _done(load_library().ssd_add_norm_backward(
-            ctypes.byref(prob), _ptr(dy), _ptr(residual), _ptr(weight), _ptr(dresidual), _ptr(dx),
-            None if dr is dx else _ptr(dr), _ptr(g["dweight"]), _ptr(workspace), need, _stream(on)),
-            "ssd_add_norm_backward")
+    _launch(dy.get_device(), "ssd_add_norm_backward", prob, _ptr(dy), _ptr(residual), _ptr(weight), _ptr(dresidual),
+            _ptr(dx), None if dr is dx else _ptr(dr), _ptr(g["dweight"]), _ptr(workspace), need)
     return g
