@@ -312,24 +312,12 @@ __global__ __launch_bounds__(64 * kWaves) void k_conv_backward(ConvParams p, int
     }
 }
 
-// dweight and dbias: the strips' partial sums, in order, 16 interleaved sums per
-// column joined at the end.
-constexpr int kSumLanes = 16, kSumCols = 16;
-
+// dweight and dbias: the strips' partial sums, in a fixed order.
 __global__ __launch_bounds__(kSumLanes * kSumCols) void k_conv_dw(ConvParams p, int64_t strips)
 {
-    __shared__ float part[kSumLanes][kSumCols + 1];
-    const int col = threadIdx.x % kSumCols, lane = threadIdx.x / kSumCols;
-    const int64_t cols = (p.W + 1) * p.C, i = static_cast<int64_t>(blockIdx.x) * kSumCols + col;
-    float v = 0.f;
-    if (i < cols)
-        for (int64_t s = lane; s < strips; s += kSumLanes) v += p.partial[s * cols + i];
-    part[lane][col] = v;
-    __syncthreads();
-    if (lane != 0 || i >= cols) return;
-    v = 0.f;
-#pragma unroll
-    for (int k = 0; k < kSumLanes; ++k) v += part[k][col];
+    const int64_t cols = (p.W + 1) * p.C, i = static_cast<int64_t>(blockIdx.x) * kSumCols + threadIdx.x % kSumCols;
+    const float v = column_sum(p.partial + i, strips, cols, i < cols);
+    if (threadIdx.x >= kSumCols || i >= cols) return;
     const int64_t j = i / p.C, c = i - j * p.C;
     if (j < p.W)
         p.dweight[c * p.W + j] = v;

@@ -332,23 +332,11 @@ __global__ __launch_bounds__(kBlock<LANES>) void k_add_norm_backward(NormParams 
     }
 }
 
-constexpr int kSumLanes = 16, kSumCols = 16;
-
 __global__ __launch_bounds__(kSumLanes * kSumCols) void k_norm_dw(const float* partial, int64_t rows, int64_t C, float* dw)
 {
-    __shared__ float part[kSumLanes][kSumCols + 1];
-    const int col = threadIdx.x % kSumCols, lane = threadIdx.x / kSumCols;
-    const int64_t c = static_cast<int64_t>(blockIdx.x) * kSumCols + col;
-    float v = 0.f;
-    if (c < C)
-        for (int64_t s = lane; s < rows; s += kSumLanes) v += partial[s * C + c];
-    part[lane][col] = v;
-    __syncthreads();
-    if (lane != 0 || c >= C) return;
-    v = 0.f;
-#pragma unroll
-    for (int k = 0; k < kSumLanes; ++k) v += part[k][col];
-    dw[c] = v;
+    const int64_t c = static_cast<int64_t>(blockIdx.x) * kSumCols + threadIdx.x % kSumCols;
+    const float v = column_sum(partial + c, rows, C, c < C);
+    if (threadIdx.x < kSumCols && c < C) dw[c] = v;
 }
 
 // Lanes a row: a wavefront where rows are many and short enough for its

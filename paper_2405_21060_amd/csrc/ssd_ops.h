@@ -186,6 +186,32 @@ struct Pack<T, 1> {
     __device__ __forceinline__ void store(T* p) const { *p = v; }
 };
 
+// The sum of a column of partial sums, `rows` values `step` apart: kSumLanes
+// threads take every kSumLanes-th value, in four sums of their own, and join in
+// order.  A workgroup takes kSumCols columns; the sum is thread (lane 0, col)'s.
+constexpr int kSumLanes = 64, kSumCols = 16;
+
+__device__ __forceinline__ float column_sum(const float* from, int64_t rows, int64_t step, bool real)
+{
+    __shared__ float part[kSumLanes][kSumCols + 1];
+    const int col = threadIdx.x % kSumCols, lane = threadIdx.x / kSumCols;
+    float v[4] = {};
+    if (real)
+        for (int64_t k = lane; k < rows; k += 4 * kSumLanes) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (k + u * kSumLanes < rows) v[u] += from[(k + u * kSumLanes) * step];
+        }
+    part[lane][col] = (v[0] + v[1]) + (v[2] + v[3]);
+    __syncthreads();
+    float sum = 0.f;
+    if (lane == 0) {
+#pragma unroll 8
+        for (int k = 0; k < kSumLanes; ++k) sum += part[k][col];
+    }
+    return sum;
+}
+
 #endif
 
 }  // namespace ssd

@@ -253,47 +253,79 @@ __global__ __launch_bounds__(256) void k_scan_pass(ScanParams p)
 }
 
 // One token per batch row.  Memory-bound: the state is read and written once.  A
-// thread owns 4 consecutive states (16 bytes), the N / 4 threads of a channel are
-// a power-of-two segment of a wavefront.
-template <typename T>
+// thread owns 4 consecutive states (16 bytes) of ROWS batch rows, the N / 4 threads
+// of a channel are a power-of-two segment of a wavefront.  Several rows a thread
+// share A and have their loads in flight together.
+template <typename T, int ROWS>
 __global__ __launch_bounds__(256) void k_scan_step(ScanParams p, int seg, int log2seg)
 {
     const int64_t i = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) >> log2seg;
     const int n0 = 4 * (threadIdx.x & (seg - 1));
-    const bool live = i < p.b * p.E && n0 < p.N;
-    float sum = 0.f, xv = 0.f;
-    int64_t row = 0, e = 0;
+    const int64_t block = i / p.E, e = i - block * p.E, row0 = block * ROWS;
+    const bool live = row0 < p.b && n0 < p.N;
+    typedef float f4 __attribute__((ext_vector_type(4)));
+    float sum[ROWS] = {}, xv[ROWS] = {};
     if (live) {
-        row = i / p.E;
-        e = i - row * p.E;
         const int64_t g = e / (p.E / p.G);
-        const T* B = static_cast<const T*>(p.B) + row * p.bb + g * p.N + n0;
-        const T* C = static_cast<const T*>(p.C) + row * p.cb + g * p.N + n0;
-        float* st = p.fin + i * p.N + n0;
-        const float4 old = *reinterpret_cast<const float4*>(st);
-        const auto a = Pack<float, 4>::load(p.A_log + e * p.N + n0);
-        const auto b = Pack<T, 4>::load(B), c = Pack<T, 4>::load(C);
-        xv = widen(static_cast<const T*>(p.x)[row * p.xb + e]);
-        const float d = time_step(p, widen(static_cast<const T*>(p.dt)[row * p.db + e]) + (p.dt_bias ? p.dt_bias[e] : 0.f));
-        const float in = d * xv, o[4] = {old.x, old.y, old.z, old.w};
-        float h[4];
+        const T* B = static_cast<const T*>(p.B) + g * p.N + n0;
+        const T* C = static_cast<const T*>(p.C) + g * p.N + n0;
+        const T* x = static_cast<const T*>(p.x) + e;
+        const T* dt = static_cast<const T*>(p.dt) + e;
+        f4 st[ROWS];
+        Pack<T, 4> b[ROWS], c[ROWS];
+        float d[ROWS];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            h[k] = fmaf(__builtin_amdgcn_exp2f(d * decay_rate(a[k])), o[k], in * b[k]);
-            sum = fmaf(h[k], c[k], sum);
+        for (int r = 0; r < ROWS; ++r) {
+            const int64_t row = row0 + r < p.b ? row0 + r : p.b - 1;
+            st[r] = *reinterpret_cast<const f4*>(p.fin + (row * p.E + e) * p.N + n0);
+            xv[r] = widen(x[row * p.xb]);
+            d[r] = widen(dt[row * p.db]);
+            b[r] = Pack<T, 4>::load(B + row * p.bb);
+            c[r] = Pack<T, 4>::load(C + row * p.cb);
         }
-        typedef float f4 __attribute__((ext_vector_type(4)));
-        __builtin_nontemporal_store(f4{h[0], h[1], h[2], h[3]}, reinterpret_cast<f4*>(st));
+        const auto a = Pack<float, 4>::load(p.A_log + e * p.N + n0);
+        const float bias = p.dt_bias ? p.dt_bias[e] : 0.f;
+        float A2[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) A2[k] = decay_rate(a[k]);
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            const float dv = time_step(p, d[r] + bias), in = dv * xv[r];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                st[r][k] = fmaf(__builtin_amdgcn_exp2f(dv * A2[k]), st[r][k], in * b[r][k]);
+                sum[r] = fmaf(st[r][k], c[r][k], sum[r]);
+            }
+            if (row0 + r < p.b)
+                __builtin_nontemporal_store(st[r], reinterpret_cast<f4*>(p.fin + ((row0 + r) * p.E + e) * p.N + n0));
+        }
     }
-    for (int off = seg >> 1; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
-    if (live && n0 == 0) {
-        if (p.D) sum = fmaf(p.D[e], xv, sum);
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+        for (int off = seg >> 1; off > 0; off >>= 1) sum[r] += __shfl_xor(sum[r], off, 64);
+        if (!live || n0 != 0 || row0 + r >= p.b) continue;
+        const int64_t row = row0 + r;
+        float v = p.D ? fmaf(p.D[e], xv[r], sum[r]) : sum[r];
         if (p.z) {
             const float zv = widen(static_cast<const T*>(p.z)[row * p.zb + e]);
-            sum *= zv * sigmoid_hw(zv);
+            v *= zv * sigmoid_hw(zv);
         }
-        static_cast<T*>(p.y)[i] = narrow<T>(sum);
+        static_cast<T*>(p.y)[row * p.E + e] = narrow<T>(v);
     }
+}
+
+template <typename T, int ROWS>
+hipError_t step(const ScanParams& p, hipStream_t stream)
+{
+    int seg = 4, log2seg = 2;
+    while (4 * seg < p.N) {
+        seg <<= 1;
+        ++log2seg;
+    }
+    const int64_t grid = ((p.b + ROWS - 1) / ROWS * p.E * seg + 255) / 256;
+    if (grid > kMaxGrid) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL((k_scan_step<T, ROWS>), dim3(static_cast<unsigned>(grid)), dim3(256), 0, stream, p, seg, log2seg);
+    return hipGetLastError();
 }
 
 template <typename T, bool PACKED, Mode MODE, int THREADS>
@@ -394,18 +426,10 @@ hipError_t launch_scan_forward(const ScanParams& p, bool bf16, hipStream_t strea
 
 hipError_t launch_scan_step(const ScanParams& p, bool bf16, hipStream_t stream)
 {
-    int seg = 4, log2seg = 2;
-    while (4 * seg < p.N) {
-        seg <<= 1;
-        ++log2seg;
-    }
-    const int64_t grid = (p.b * p.E * seg + 255) / 256;
-    if (grid > kMaxGrid) return hipErrorInvalidConfiguration;
-    if (bf16)
-        hipLaunchKernelGGL(k_scan_step<uint16_t>, dim3(static_cast<unsigned>(grid)), dim3(256), 0, stream, p, seg, log2seg);
-    else
-        hipLaunchKernelGGL(k_scan_step<float>, dim3(static_cast<unsigned>(grid)), dim3(256), 0, stream, p, seg, log2seg);
-    return hipGetLastError();
+    // four rows a thread where that leaves the device 4,096 wavefronts
+    const bool four = p.b >= 4 && p.b / 4 * p.E * (p.N / 4) >= 4096 * 64;
+    if (bf16) return four ? step<uint16_t, 4>(p, stream) : step<uint16_t, 1>(p, stream);
+    return four ? step<float, 4>(p, stream) : step<float, 1>(p, stream);
 }
 
 }  // namespace ssd

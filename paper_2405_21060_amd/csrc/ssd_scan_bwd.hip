@@ -419,27 +419,14 @@ __global__ __launch_bounds__(64, 2) void k_scan_grad(ScanParams p)
     p.pD[(rc * 2 + 1) * p.E + w.e] = sumBias;
 }
 
-// dA_log, dD and ddt_bias: sums over rows and chunks, 32 interleaved ones a
-// column joined at the end.
-constexpr int kSumLanes = 32, kSumCols = 32;
-
+// dA_log, dD and ddt_bias: sums over rows and chunks, in a fixed order.
 __global__ __launch_bounds__(kSumLanes * kSumCols) void k_scan_sum_params(ScanParams p)
 {
-    __shared__ float part[kSumLanes][kSumCols + 1];
-    const int col = threadIdx.x % kSumCols, lane = threadIdx.x / kSumCols;
-    const int64_t i = static_cast<int64_t>(blockIdx.x) * kSumCols + col, ne = p.N * p.E, parts = p.b * p.S;
-    const bool first = i < ne;   // (N E is a multiple of 16: a column of dA or one of dD, ddt_bias)
-    const float* from = first ? p.pA + i : p.pD + (i - ne);
-    const int64_t step = first ? ne : 2 * p.E;
-    float v = 0.f;
-    if (i < ne + 2 * p.E)
-        for (int64_t k = lane; k < parts; k += kSumLanes) v += from[k * step];
-    part[lane][col] = v;
-    __syncthreads();
-    if (lane != 0 || i >= ne + 2 * p.E) return;
-    v = 0.f;
-#pragma unroll
-    for (int k = 0; k < kSumLanes; ++k) v += part[k][col];
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * kSumCols + threadIdx.x % kSumCols;
+    const int64_t ne = p.N * p.E, all = ne + 2 * p.E;
+    const bool first = i < ne;   // a column of dA, else one of dD or ddt_bias
+    const float v = column_sum(first ? p.pA + i : p.pD + (i - ne), p.b * p.S, first ? ne : 2 * p.E, i < all);
+    if (threadIdx.x >= kSumCols || i >= all) return;
     if (first) {
         const int64_t n = i / p.E, e = i - n * p.E;
         p.dA_log[e * p.N + n] = v * (decay_rate(p.A_log[e * p.N + n]) * 0.69314718f);
