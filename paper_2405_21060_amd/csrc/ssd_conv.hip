@@ -7,7 +7,9 @@
 //
 // Bound by HBM: x is read and y written once (gradients: x and dy read, dx
 // written).  A wavefront takes a strip of consecutive tokens of 64 x V channels
-// (V = 4, a vector per lane) and walks down the tokens with the W - 1 rows
+// (V = 2 a lane; 4 and 8 hold more registers and leave fewer wavefronts: forward 4 x
+// 4,096 x 5,376 bf16 76 us, 84 and 92, gradients 1 x 32,768 x 6,144 283, 289 and
+// 333) and walks down the tokens with the W - 1 rows
 // before the present one in registers, so that a token's row is read once, and
 // the W - 1 rows in front of a strip once more.  Sequences of a packed row are the
 // wavefront's own control flow: at a sequence's first token the rows in
@@ -359,16 +361,18 @@ int64_t channel_tiles(const ConvParams& p, int V)
     return n;
 }
 
-// Vectors of 4 channels, where every part has that many.
+// Vectors of two channels, where every part has that many.
 bool vectors(const ConvParams& p)
 {
     for (int i = 0; i < p.nparts; ++i)
-        if (p.off[i + 1] - p.off[i] < 4) return false;
+        if (p.off[i + 1] - p.off[i] < 2) return false;
     return true;
 }
 
 // Tokens per strip: longer strips read fewer rows twice, shorter ones give more
-// wavefronts; the longest that leaves 4,096 (four a SIMD), else the shortest.
+// wavefronts; the longest that leaves 4,096 (four a SIMD), else the shortest.  The
+// longest is 32 tokens (64: 80 us for the forward above) and 128 for the gradients
+// (64: 295 us), whose strips have a row of partial sums each.
 int64_t strip_tokens(int64_t b, int64_t T, int64_t tiles, int64_t longest, int64_t shortest)
 {
     int64_t R = longest;
@@ -395,7 +399,7 @@ hipError_t run(const ConvParams& p, int64_t R, bool backward, hipStream_t stream
 template <typename T, int W>
 hipError_t by_vector(const ConvParams& p, int64_t R, bool backward, hipStream_t stream)
 {
-    if (vectors(p)) return p.seq_idx ? run<T, W, 4, true>(p, R, backward, stream) : run<T, W, 4, false>(p, R, backward, stream);
+    if (vectors(p)) return p.seq_idx ? run<T, W, 2, true>(p, R, backward, stream) : run<T, W, 2, false>(p, R, backward, stream);
     return p.seq_idx ? run<T, W, 1, true>(p, R, backward, stream) : run<T, W, 1, false>(p, R, backward, stream);
 }
 
@@ -431,11 +435,11 @@ hipError_t step_by_width(const ConvParams& p, hipStream_t stream)
 }  // namespace
 
 // (by the channels alone, not by the parts: the workspace depends on it)
-int64_t conv_bwd_strip(int64_t b, int64_t T, int64_t C) { return strip_tokens(b, T, (C + 255) / 256, 128, 16); }
+int64_t conv_bwd_strip(int64_t b, int64_t T, int64_t C) { return strip_tokens(b, T, (C + 127) / 128, 128, 16); }
 
 hipError_t launch_conv_forward(const ConvParams& p, bool bf16, hipStream_t stream)
 {
-    const int64_t R = strip_tokens(p.b, p.T, channel_tiles(p, vectors(p) ? 4 : 1), 64, 4);
+    const int64_t R = strip_tokens(p.b, p.T, channel_tiles(p, vectors(p) ? 2 : 1), 32, 4);
     return bf16 ? by_width<uint16_t>(p, R, false, stream) : by_width<float>(p, R, false, stream);
 }
 
