@@ -53,6 +53,7 @@ struct ScanParams {
     int64_t S, L;
     float* states;
     float* sums;
+    float* steps;                        // time steps (b, T, E) (forward)
     // gradients
     const void* dy;
     const float* dfin;
@@ -68,7 +69,7 @@ struct ScanParams {
 
 struct ScanPlan {
     int64_t S, L;
-    size_t states, sums, rstates, marks, marksums, pA, pD, pBC, total;   // byte offsets
+    size_t states, sums, steps, rstates, marks, marksums, pA, pD, pBC, total;   // byte offsets
     int64_t cblocks;   // channel blocks of the gradients
 };
 

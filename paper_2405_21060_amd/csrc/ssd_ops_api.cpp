@@ -145,6 +145,7 @@ void place(const ssd::ScanPlan& w, void* workspace, ssd::ScanParams* p)
     p->L = w.L;
     p->states = at(w.states);
     p->sums = at(w.sums);
+    p->steps = at(w.steps);
     p->rstates = at(w.rstates);
     p->marks = at(w.marks);
     p->marksums = at(w.marksums);

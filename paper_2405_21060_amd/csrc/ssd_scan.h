@@ -77,6 +77,17 @@ __device__ __forceinline__ bool scan_ends(const ScanParams& p, int64_t t)
 template <typename P>
 __device__ __forceinline__ void running(P& p) { asm volatile("" : "+s"(p)); }
 
+// A lane's offset in a row of T, made where it is used: a load or store then adds
+// the 32-bit offset to the scalar pointer itself (widened ahead of a loop, it takes a
+// 64-bit addition for every access).
+template <typename T>
+__device__ __forceinline__ unsigned lane_offset(unsigned lane)
+{
+    unsigned off = lane * sizeof(T);
+    asm volatile("" : "+v"(off));
+    return off;
+}
+
 // A tensor's row of a token, walked from token to token: a uniform pointer and the
 // lane's offset.
 template <typename T>
@@ -87,8 +98,14 @@ struct Rows {
 
     __device__ __forceinline__ Rows(const void* base, int64_t first, int64_t stride)
         : p((pointer)(reinterpret_cast<uintptr_t>(base) + first * sizeof(T))), step(static_cast<int>(stride)) {}
-    __device__ __forceinline__ T get(unsigned lane) const { return p[lane]; }
-    __device__ __forceinline__ void put(unsigned lane, T v) const { p[lane] = v; }
+    // `off`: the lane's offset in bytes (lane_offset)
+    __device__ __forceinline__ pointer at(unsigned off) const
+    {
+        typedef __attribute__((address_space(1))) char* bytes;
+        return (pointer)((bytes)p + off);
+    }
+    __device__ __forceinline__ T get(unsigned off) const { return *at(off); }
+    __device__ __forceinline__ void put(unsigned off, T v) const { *at(off) = v; }
     __device__ __forceinline__ void move(bool on = true)
     {
         p += on ? step : 0;

@@ -13,18 +13,21 @@
 // tiles alone do not fill the device, the tokens are cut into chunks of L: their
 // states from zero (k_scan_chunk<kStates>), a scan over the chunks
 // (k_scan_pass), then the outputs from each chunk's entering state
-// (k_scan_chunk<kOutput>); the first of the three costs five more slots.
+// (k_scan_chunk<kOutputReady>); the first of the three costs five more slots.
 // Sequences of a packed row replace the state at their first token.
+#include <type_traits>
+
 #include "ssd_internal.h"
 #include "ssd_scan.h"
 
 namespace ssd {
 namespace {
 
-enum Mode { kOutput, kStates, kBoth };
+enum Mode { kOutput, kOutputReady, kStates, kBoth };
 
 // kOutput: y and final states.  kStates: each chunk's state from zero (from the
-// initial state in the first one) and its sum of dt.  For the gradients, kBoth: that,
+// initial state in the first one), its sum of dt, and the time steps themselves,
+// which kOutputReady then takes as they are (13 instructions of 128 a token).  For the gradients, kBoth: that,
 // and the gradient of the state entering each chunk from the chunk's own outputs,
 // sum_t exp(A sum_{s <= t} dt_s) dy~_t C_t (walked forwards too, the product of the
 // decays so far kept: one exp2 serves both), and in front of every tile of kBwdTile
@@ -36,26 +39,26 @@ enum Mode { kOutput, kStates, kBoth };
 // before they are needed.  With several wavefronts their shares
 // of y meet in shared memory, and wavefront k finishes every token u = k, k +
 // slices, ..
-template <typename T, bool PACKED, Mode MODE, int THREADS>
+template <typename T, bool PACKED, bool GATE, Mode MODE, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_scan_chunk(ScanParams p)
 {
-    extern __shared__ float shared[];   // kOutput with several wavefronts: [2][kTok][slices][64]
-    constexpr bool kOne = THREADS == 64, kOut = MODE == kOutput, kBack = MODE == kBoth;
+    extern __shared__ float shared[];   // outputs with several wavefronts: [2][kTok][slices][64]
+    constexpr bool kOne = THREADS == 64, kReady = MODE == kOutputReady, kOut = MODE == kOutput || kReady;
+    constexpr bool kBack = MODE == kBoth;
     const int slice = kOne ? 0 : uniform(threadIdx.x >> 6);
     const int slices = kOne ? 1 : static_cast<int>(p.N / kSlice);
     const unsigned col = threadIdx.x & 63;
     const ScanWork w = scan_work(p, blockIdx.x);
-    if (MODE == kStates && w.chunk == p.S - 1) return;   // no chunk after it
     const int n0 = slice * kSlice;
-    const bool gate = (kOut || kBack) && p.z;
     Rows<const T> x(p.x, w.row * p.xb + w.t0 * p.xt + w.e0, p.xt);
     Rows<const T> dt(p.dt, w.row * p.db + w.t0 * p.dtt + w.e0, p.dtt);
-    Rows<const T> z(gate ? p.z : p.x, gate ? w.row * p.zb + w.t0 * p.zt + w.e0 : 0, gate ? p.zt : 0);
+    Rows<const T> z(GATE ? p.z : p.x, GATE ? w.row * p.zb + w.t0 * p.zt + w.e0 : 0, GATE ? p.zt : 0);
     Rows<const T> B(p.B, w.row * p.bb + w.t0 * p.bt + w.g * p.N + n0, p.bt);
     Rows<const T> C(p.C, w.row * p.cb + w.t0 * p.ct + w.g * p.N + n0, p.ct);
     const int64_t out = (w.row * p.T + w.t0) * p.E + w.e0;
     Rows<T> y(p.y, out, p.E);
     Rows<const T> dy(kBack ? p.dy : p.x, kBack ? out : 0, kBack ? p.E : 0);
+    Rows<float> steps(p.steps, out, p.E);
     float A2[kSlice], h[kSlice];
     float cum[kSlice], r[kSlice];   // kBoth: decay since the chunk's start, gradient so far
 #pragma unroll
@@ -83,18 +86,26 @@ __global__ __launch_bounds__(THREADS) void k_scan_chunk(ScanParams p)
 
     const int count = static_cast<int>(w.t1 - w.t0);
     int ahead = 0;   // the token that the pointers of x, dt and z are at
-    T xr[kTok], dr[kTok], zr[kTok], yr[kTok];
-    const auto fetch = [&]() {
+    T xr[kTok], zr[kTok] = {}, yr[kTok];
+    std::conditional_t<kReady, float, T> dr[kTok];
+    const auto fetch = [&]() __attribute__((always_inline)) {
+        const unsigned off = lane_offset<T>(w.lane), off4 = lane_offset<float>(w.lane);
 #pragma unroll
         for (int u = 0; u < kTok; ++u) {
-            xr[u] = x.get(w.lane);
-            dr[u] = dt.get(w.lane);
-            if (gate) zr[u] = z.get(w.lane);
-            if (kBack) yr[u] = dy.get(w.lane);
+            xr[u] = x.get(off);
+            if constexpr (kReady)
+                dr[u] = steps.get(off4);
+            else
+                dr[u] = dt.get(off);
+            if (GATE) zr[u] = z.get(off);
+            if (kBack) yr[u] = dy.get(off);
             const bool more = ++ahead < count;   // (at the end: the last token again)
             x.move(more);
-            dt.move(more);
-            if (gate) z.move(more);
+            if constexpr (kReady)
+                steps.move(more);
+            else
+                dt.move(more);
+            if (GATE) z.move(more);
             if (kBack) dy.move(more);
         }
     };
@@ -104,7 +115,7 @@ __global__ __launch_bounds__(THREADS) void k_scan_chunk(ScanParams p)
     if (kOut || kBack) cn.load(C);
     // kBoth: the unit's sequence ends here; its final state's gradient counts too.
     bool open = true;   // no sequence has ended in the chunk yet
-    const auto leave = [&]() {
+    const auto leave = [&]() __attribute__((always_inline)) {
         if (!open) return;
         open = false;
         float f[kSlice];
@@ -113,31 +124,35 @@ __global__ __launch_bounds__(THREADS) void k_scan_chunk(ScanParams p)
         for (int n = 0; n < kSlice; ++n) r[n] = fmaf(cum[n], f[n], r[n]);
     };
     float* part = shared;
-    for (int t = 0; t < count; t += kTok) {
+    // A tile from token t of the chunk on; FULL: all of its tokens are the chunk's.
+    const auto tile = [&](int t, auto full) __attribute__((always_inline)) {
+        constexpr bool FULL = decltype(full)::value;
         static_assert(kTok == kBwdTile, "a mark in front of every tile");
         if (kBack && w.live) {
-            const int64_t tile = w.row * ((p.T + kBwdTile - 1) / kBwdTile) + (w.t0 + t) / kBwdTile;
-            float* m = p.marks + (tile * p.N + n0) * p.E + w.e;
+            const int64_t at = w.row * ((p.T + kBwdTile - 1) / kBwdTile) + (w.t0 + t) / kBwdTile;
+            float* m = p.marks + (at * p.N + n0) * p.E + w.e;
 #pragma unroll
             for (int n = 0; n < kSlice; ++n) m[n * p.E] = h[n];
-            if (slice == 0) p.marksums[tile * p.E + w.e] = sum;
+            if (slice == 0) p.marksums[at * p.E + w.e] = sum;
         }
         float xv[kTok], d[kTok], zv[kTok], dyg[kTok];
 #pragma unroll
         for (int u = 0; u < kTok; ++u) {
             xv[u] = widen(xr[u]);
-            zv[u] = gate ? widen(zr[u]) : 0.f;
-            d[u] = widen(dr[u]) + bias;
-            if (kBack) dyg[u] = gate ? widen(yr[u]) * zv[u] * sigmoid_hw(zv[u]) : widen(yr[u]);
+            zv[u] = GATE ? widen(zr[u]) : 0.f;
+            if (kBack) dyg[u] = GATE ? widen(yr[u]) * zv[u] * sigmoid_hw(zv[u]) : widen(yr[u]);
         }
-        fetch();   // the next tile's
-        if (p.softplus) {
+#pragma unroll
+        for (int u = 0; u < kTok; ++u) d[u] = kReady ? widen(dr[u]) : widen(dr[u]) + bias;
+        if (!kReady && p.softplus) {
 #pragma unroll
             for (int u = 0; u < kTok; ++u) d[u] = softplus_hw(d[u]);
         }
+        fetch();   // the next tile's
+        const unsigned off = lane_offset<T>(w.lane), off4 = lane_offset<float>(w.lane);
 #pragma unroll
         for (int u = 0; u < kTok; ++u) {
-            if (t + u >= count) break;
+            if (!FULL && t + u >= count) break;
             if (PACKED) {
                 if (w.t0 + t + u > 0 && scan_starts<PACKED>(p, w.t0 + t + u)) {
                     // (from the first start behind the chunk's first token on, nothing
@@ -160,6 +175,10 @@ __global__ __launch_bounds__(THREADS) void k_scan_chunk(ScanParams p)
             }
             __builtin_amdgcn_sched_barrier(0);   // the loads stay in front of the token's arithmetic
             if (MODE == kStates || kBack) sum += d[u];
+            if (MODE == kStates && slice == 0) {   // (a lane past its group's end: the last one's value again)
+                steps.put(off4, d[u]);
+                steps.move();
+            }
             float ys[2] = {0.f, 0.f};
 #pragma unroll
             for (int n = 0; n < kSlice; ++n) {
@@ -176,8 +195,8 @@ __global__ __launch_bounds__(THREADS) void k_scan_chunk(ScanParams p)
                     store_states(p.fin, p, unit, w.e, n0, h);
                 if (kOne) {
                     float v = fmaf(D, xv[u], ys[0] + ys[1]);
-                    if (gate) v *= zv[u] * sigmoid_hw(zv[u]);
-                    if (w.live) y.put(w.lane, narrow<T>(v));
+                    if (GATE) v *= zv[u] * sigmoid_hw(zv[u]);
+                    y.put(off, narrow<T>(v));   // (so is y)
                     y.move();
                 } else {
                     part[(u * slices + slice) * 64 + col] = ys[0] + ys[1];
@@ -188,20 +207,23 @@ __global__ __launch_bounds__(THREADS) void k_scan_chunk(ScanParams p)
             __syncthreads();
 #pragma unroll
             for (int u = 0; u < kTok; ++u) {
-                if (t + u >= count) break;
+                if (!FULL && t + u >= count) break;
                 if (u % slices == slice) {
                     float v = 0.f;
                     for (int k = 0; k < slices; ++k) v += part[(u * slices + k) * 64 + col];
                     v = fmaf(D, xv[u], v);
-                    if (gate) v *= zv[u] * sigmoid_hw(zv[u]);
-                    if (w.live) y.put(w.lane, narrow<T>(v));
+                    if (GATE) v *= zv[u] * sigmoid_hw(zv[u]);
+                    y.put(lane_offset<T>(w.lane), narrow<T>(v));
                 }
                 y.move();
             }
             // (the other half is written next, so one barrier a tile is enough)
             part = part == shared ? shared + kTok * slices * 64 : shared;
         }
-    }
+    };
+    int t = 0;
+    for (; t + kTok <= count; t += kTok) tile(t, std::true_type{});
+    if (t < count) tile(t, std::false_type{});
     if (kOut && !PACKED && p.fin && w.live && w.t1 == p.T) store_states(p.fin, p, unit, w.e, n0, h);
     if (kBack && scan_ends<PACKED>(p, w.t1 - 1)) leave();
     if ((MODE == kStates || kBack) && w.live && p.S > 1) {
@@ -328,30 +350,38 @@ hipError_t step(const ScanParams& p, hipStream_t stream)
     return hipGetLastError();
 }
 
-template <typename T, bool PACKED, Mode MODE, int THREADS>
+template <typename T, bool PACKED, bool GATE, Mode MODE, int THREADS>
 hipError_t chunk(const ScanParams& p, hipStream_t stream)
 {
     const int64_t units = p.b * p.S * p.G * scan_tiles(p.E, p.G);
     const int slices = static_cast<int>(p.N / kSlice);
-    const size_t lds = MODE == kOutput && slices > 1 ? 2 * kTok * slices * 64 * sizeof(float) : 0;
+    const size_t lds = (MODE == kOutput || MODE == kOutputReady) && slices > 1 ? 2 * kTok * slices * 64 * sizeof(float) : 0;
     if (units > kMaxGrid) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL((k_scan_chunk<T, PACKED, MODE, THREADS>), dim3(static_cast<unsigned>(units)), dim3(64 * slices),
+    hipLaunchKernelGGL((k_scan_chunk<T, PACKED, GATE, MODE, THREADS>), dim3(static_cast<unsigned>(units)), dim3(64 * slices),
                        lds, stream, p);
     return hipGetLastError();
 }
 
-template <typename T, bool PACKED, Mode MODE>
+template <typename T, bool PACKED, bool GATE, Mode MODE>
 hipError_t by_states(const ScanParams& p, hipStream_t stream)
 {
-    if (p.N <= kSlice) return chunk<T, PACKED, MODE, 64>(p, stream);
-    if (p.N <= 4 * kSlice) return chunk<T, PACKED, MODE, 256>(p, stream);
-    return chunk<T, PACKED, MODE, 1024>(p, stream);
+    if (p.N <= kSlice) return chunk<T, PACKED, GATE, MODE, 64>(p, stream);
+    if (p.N <= 4 * kSlice) return chunk<T, PACKED, GATE, MODE, 256>(p, stream);
+    return chunk<T, PACKED, GATE, MODE, 1024>(p, stream);
+}
+
+template <typename T, bool PACKED, Mode MODE>
+hipError_t by_gate(const ScanParams& p, hipStream_t stream)
+{
+    if constexpr (MODE != kStates)
+        if (p.z) return by_states<T, PACKED, true, MODE>(p, stream);
+    return by_states<T, PACKED, false, MODE>(p, stream);
 }
 
 template <typename T, Mode MODE>
 hipError_t chunks(const ScanParams& p, hipStream_t stream)
 {
-    return p.seq_idx ? by_states<T, true, MODE>(p, stream) : by_states<T, false, MODE>(p, stream);
+    return p.seq_idx ? by_gate<T, true, MODE>(p, stream) : by_gate<T, false, MODE>(p, stream);
 }
 
 }  // namespace
@@ -401,7 +431,10 @@ ScanPlan scan_plan(int64_t b, int64_t T, int64_t E, int64_t N, int64_t G, bool b
     if (w.S > 1) {
         w.states = take(st);
         w.sums = take(b * w.S * E);
-        if (backward) w.rstates = take(st);
+        if (backward)
+            w.rstates = take(st);
+        else
+            w.steps = take(b * T * E);
     }
     if (backward) {
         w.marks = take(b * ((T + kBwdTile - 1) / kBwdTile) * N * E);
@@ -420,6 +453,7 @@ hipError_t launch_scan_forward(const ScanParams& p, bool bf16, hipStream_t strea
         hipError_t err = bf16 ? chunks<uint16_t, kStates>(p, stream) : chunks<float, kStates>(p, stream);
         if (err == hipSuccess) err = launch_scan_pass(p, stream);
         if (err != hipSuccess) return err;
+        return bf16 ? chunks<uint16_t, kOutputReady>(p, stream) : chunks<float, kOutputReady>(p, stream);
     }
     return bf16 ? chunks<uint16_t, kOutput>(p, stream) : chunks<float, kOutput>(p, stream);
 }

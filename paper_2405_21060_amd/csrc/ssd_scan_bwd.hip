@@ -183,12 +183,13 @@ __device__ __forceinline__ void grad_tile(const ScanParams& p, const ScanWork& w
         Rows<const T> z(GATE ? p.z : p.x, GATE ? w.row * p.zb + t0 * p.zt + w.e0 : 0, GATE ? p.zt : 0);
         Rows<const T> dy(p.dy, out, p.E);
         T xr[kBwdTile], dr[kBwdTile], yr[kBwdTile], zr[kBwdTile];
+        const unsigned off = lane_offset<T>(w.lane);
 #pragma unroll
         for (int u = 0; u < kBwdTile; ++u) {
-            xr[u] = x.get(w.lane);
-            dr[u] = dt.get(w.lane);
-            yr[u] = dy.get(w.lane);
-            if (GATE) zr[u] = z.get(w.lane);
+            xr[u] = x.get(off);
+            dr[u] = dt.get(off);
+            yr[u] = dy.get(off);
+            if (GATE) zr[u] = z.get(off);
             const bool more = FULL || u + 1 < count;   // (at the end: the last token again)
             if (u + 1 == kBwdTile) break;
             x.move(more);
@@ -246,16 +247,18 @@ __device__ __forceinline__ void grad_tile(const ScanParams& p, const ScanWork& w
     float4 al;
     float mn[kQuad], en[kQuad] = {};
     const auto ahead = [&](int q) {
+        unsigned off = lane_offset<float>(w.lane);
         al = *reinterpret_cast<const float4*>(A_log + q);
 #pragma unroll
         for (int n = 0; n < kQuad; ++n) {
-            mn[n] = m.get(w.lane);
+            mn[n] = m.get(off);
             m.move();
         }
         if (reached) {
+            off = lane_offset<float>(w.lane);
 #pragma unroll
             for (int n = 0; n < kQuad; ++n) {
-                en[n] = entering.get(w.lane);
+                en[n] = entering.get(off);
                 entering.move();
             }
         }
@@ -375,9 +378,10 @@ __device__ __forceinline__ void grad_tile(const ScanParams& p, const ScanWork& w
             sumD = fmaf(dyg[u], xv[u], sumD);
             sumBias += dd;
             if (w.live) {
-                dx.put(w.lane, narrow<T>(fmaf(d[u], du[u], D * dyg[u])));
-                ddt.put(w.lane, narrow<T>(dd));
-                if (GATE) dz.put(w.lane, narrow<T>(zd[u * 64] * fmaf(D, xv[u], ys[u])));
+                const unsigned off = lane_offset<T>(w.lane);
+                dx.put(off, narrow<T>(fmaf(d[u], du[u], D * dyg[u])));
+                ddt.put(off, narrow<T>(dd));
+                if (GATE) dz.put(off, narrow<T>(zd[u * 64] * fmaf(D, xv[u], ys[u])));
             }
             dx.move();
             ddt.move();
