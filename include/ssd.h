@@ -505,6 +505,7 @@ typedef struct {
     int32_t silu;
 } ssd_conv_problem;
 
+/* (strides over a single batch row or token are ignored, here and in the scan) */
 int ssd_conv_forward(const ssd_conv_problem* prob, const void* x, const float* weight, const float* bias,
                      const void* initial_states, const int32_t* seq_idx, void* const* y, void* final_states,
                      void* stream);
@@ -549,7 +550,8 @@ int ssd_conv_step(const ssd_conv_problem* prob, const void* x, const float* weig
  *   initial_states, final_states   (batch, channels, dstate) float32, 16-byte
  *                   aligned, contiguous, or NULL; (nseq, ...) with seq_idx
  * dstate is a multiple of 16 in [16, 256].  The states and all arithmetic are
- * float32; a decay below 2^-126 counts as 0.  The sequence is cut into chunks
+ * float32; a decay below 2^-126 counts as 0.  Outputs must not overlap inputs.  The
+ * sequence is cut into chunks
  * where its channels alone do not fill the device: their states from zero, a scan
  * over the chunks, then the outputs.  Workspace: ssd_scan_workspace_bytes() (for
  * the forward; may be 0).  Ownership, asynchrony, determinism and errors as for

@@ -386,7 +386,7 @@ hipError_t run(const ConvParams& p, int64_t R, bool backward, hipStream_t stream
     const int64_t strips = (p.T + R - 1) / R;
     const int64_t units = channel_tiles(p, V) * strips * p.b;
     const int64_t grid = (units + kWaves - 1) / kWaves;
-    if (grid > kMaxGrid) return hipErrorInvalidConfiguration;
+    if (!fits(grid, 64 * kWaves) || !fits((W + 1) * p.C, kSumLanes)) return hipErrorInvalidConfiguration;
     if (backward)
         hipLaunchKernelGGL((k_conv_backward<T, W, V, PACKED>), dim3(static_cast<unsigned>(grid)), dim3(64 * kWaves), 0,
                            stream, p, R, strips);
@@ -418,7 +418,7 @@ hipError_t step(const ConvParams& p, hipStream_t stream)
 {
     const int64_t n = p.C % 4 == 0 ? p.b * (p.C / 4) : p.b * p.C;
     const int64_t grid = (n + 255) / 256;
-    if (grid > kMaxGrid) return hipErrorInvalidConfiguration;
+    if (!fits(grid, 256)) return hipErrorInvalidConfiguration;
     if (p.C % 4 == 0)
         hipLaunchKernelGGL((k_conv_step<T, W, 4>), dim3(static_cast<unsigned>(grid)), dim3(256), 0, stream, p);
     else

@@ -352,7 +352,7 @@ hipError_t forward(const NormParams& p, hipStream_t stream)
 {
     constexpr int64_t per = kBlock<LANES> / LANES;
     const int64_t grid = (p.rows + per - 1) / per;
-    if (grid > kMaxGrid) return hipErrorInvalidConfiguration;
+    if (!fits(grid, kBlock<LANES>)) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL((k_add_norm<T, R, OUT, LANES, NV>), dim3(static_cast<unsigned>(grid)), dim3(kBlock<LANES>), 0,
                        stream, p);
     return hipGetLastError();

@@ -98,8 +98,8 @@ int64_t norm_bwd_partials(int64_t rows, int64_t C);
 hipError_t launch_add_norm(const NormParams& p, bool bf16, bool res_bf16, NormOut out, hipStream_t stream);
 hipError_t launch_add_norm_backward(const NormParams& p, bool bf16, bool res_bf16, hipStream_t stream);
 
-// Most workgroups of one launch (grid x, with room for its thread count in 32 bits).
-constexpr int64_t kMaxGrid = 0x7fffffffLL / 1024;
+// Whether so many workgroups of so many threads fit one launch (32 bits of threads).
+constexpr bool fits(int64_t groups, int64_t threads) { return groups <= 0xffffffffLL / threads; }
 
 #if defined(__HIP_DEVICE_COMPILE__) || defined(__HIPCC__)
 

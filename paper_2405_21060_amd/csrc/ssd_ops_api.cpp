@@ -22,7 +22,11 @@ bool known(int32_t dtype) { return dtype == SSD_DTYPE_F32 || dtype == SSD_DTYPE_
 
 size_t size_of(int32_t dtype) { return dtype == SSD_DTYPE_BF16 ? 2 : 4; }
 
-int status(hipError_t err) { return err == hipSuccess ? SSD_OK : SSD_ERR_LAUNCH; }
+// (a launcher that finds a grid too large says so before it launches anything)
+int status(hipError_t err)
+{
+    return err == hipSuccess ? SSD_OK : err == hipErrorInvalidConfiguration ? SSD_ERR_TOO_LARGE : SSD_ERR_LAUNCH;
+}
 
 // Packed rows: one row, as many sequences as fit.
 int check_packed(bool packed, int64_t batch, int64_t seqlen, int64_t nseq)
@@ -47,15 +51,15 @@ int validate_conv(const ssd_conv_problem* prob, bool packed, bool step, ssd::Con
     const int64_t T = step ? 1 : prob->seqlen;
     if (prob->batch < 1 || T < 1 || prob->channels < 1 || prob->width < 1) return SSD_ERR_BAD_SHAPE;
     if (prob->width < 2 || prob->width > 4) return SSD_ERR_UNSUPPORTED_DIMS;
-    if (prob->x_batch_stride < 0 || (!step && prob->x_token_stride < 0)) return SSD_ERR_BAD_SHAPE;
     *p = ssd::ConvParams{};
     p->b = prob->batch;
     p->T = T;
     p->C = prob->channels;
     p->W = static_cast<int>(prob->width);
     p->silu = prob->silu != 0;
-    p->xb = prob->x_batch_stride;
-    p->xt = step ? 0 : prob->x_token_stride;
+    // (strides over a single row or token play no part)
+    p->xb = p->b > 1 ? prob->x_batch_stride : 0;
+    p->xt = T > 1 ? prob->x_token_stride : 0;
     if (!step) {
         if (prob->nparts < 1 || prob->nparts > 3) return SSD_ERR_BAD_SHAPE;
         p->nparts = static_cast<int>(prob->nparts);
@@ -69,6 +73,7 @@ int validate_conv(const ssd_conv_problem* prob, bool packed, bool step, ssd::Con
         for (int i = p->nparts; i < 4; ++i) p->off[i] = at;
         if (const int rc = check_packed(packed, p->b, T, prob->nseq); rc != SSD_OK) return rc;
     }
+    if (p->xb < 0 || p->xt < 0) return SSD_ERR_BAD_SHAPE;
     p->nseq = packed ? prob->nseq : p->b;
     if (static_cast<double>(p->b) * T * p->C > kMostElems || static_cast<double>(p->nseq) * 4 * p->C > kMostElems ||
         !reaches(p->b, p->xb, T, p->xt, p->C))
@@ -100,17 +105,21 @@ int validate_scan(const ssd_scan_problem* prob, bool packed, bool step, bool z, 
     p->N = prob->dstate;
     p->G = prob->ngroups;
     p->softplus = prob->dt_softplus != 0;
-    p->xb = prob->x_batch_stride;
-    p->db = prob->dt_batch_stride;
-    p->zb = z ? prob->z_batch_stride : 0;
-    p->bb = prob->b_batch_stride;
-    p->cb = prob->c_batch_stride;
-    if (!step) {
+    if (p->b > 1) {   // (strides over a single row or token play no part)
+        p->xb = prob->x_batch_stride;
+        p->db = prob->dt_batch_stride;
+        p->zb = z ? prob->z_batch_stride : 0;
+        p->bb = prob->b_batch_stride;
+        p->cb = prob->c_batch_stride;
+    }
+    if (T > 1) {
         p->xt = prob->x_token_stride;
         p->dtt = prob->dt_token_stride;
         p->zt = z ? prob->z_token_stride : 0;
         p->bt = prob->b_token_stride;
         p->ct = prob->c_token_stride;
+    }
+    if (!step) {
         if (const int rc = check_packed(packed, p->b, T, prob->nseq); rc != SSD_OK) return rc;
     }
     for (int64_t s : {p->xb, p->xt, p->db, p->dtt, p->zb, p->zt, p->bb, p->bt, p->cb, p->ct})
@@ -122,6 +131,9 @@ int validate_scan(const ssd_scan_problem* prob, bool packed, bool step, bool z, 
         !reaches(p->b, p->zb, T, p->zt, p->E) || !reaches(p->b, p->bb, T, p->bt, p->G * p->N) ||
         !reaches(p->b, p->cb, T, p->ct, p->G * p->N))
         return SSD_ERR_TOO_LARGE;
+    // the kernels step from token to token in 32 bits
+    for (int64_t s : {p->E, p->xt, p->dtt, p->zt, p->bt, p->ct})
+        if (s > INT32_MAX) return SSD_ERR_TOO_LARGE;
     return SSD_OK;
 }
 
@@ -174,8 +186,7 @@ int validate_norm(const ssd_norm_problem* prob, ssd::NormParams* p)
     if (prob->rows < 1 || prob->channels < 1) return SSD_ERR_BAD_SHAPE;
     if (prob->channels > 32768) return SSD_ERR_UNSUPPORTED_DIMS;
     if (!(prob->eps >= 0.f) || !std::isfinite(prob->eps)) return SSD_ERR_BAD_OPTION;
-    if (static_cast<double>(prob->rows) * prob->channels > kMostElems || prob->rows > ssd::kMaxGrid)
-        return SSD_ERR_TOO_LARGE;
+    if (static_cast<double>(prob->rows) * prob->channels > kMostElems) return SSD_ERR_TOO_LARGE;
     *p = ssd::NormParams{};
     p->rows = prob->rows;
     p->C = prob->channels;

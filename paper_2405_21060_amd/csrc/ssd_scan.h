@@ -111,11 +111,6 @@ struct Rows {
         p += on ? step : 0;
         running(p);
     }
-    __device__ __forceinline__ void back(bool on = true)
-    {
-        p -= on ? step : 0;
-        running(p);
-    }
 };
 
 // K uniform values (4-byte aligned) of a row, through the scalar cache: the words
@@ -139,16 +134,6 @@ struct Uniform {
         return __uint_as_float(i % 2 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
     }
 };
-
-// K uniform values at a 4-byte aligned address, through the scalar cache.
-template <typename T, int K>
-__device__ __forceinline__ void uniform_row(const T* at, float (&v)[K])
-{
-    Uniform<T, K> u;
-    u.load(Rows<const T>(at, 0, 0));
-#pragma unroll
-    for (int i = 0; i < K; ++i) v[i] = u[i];
-}
 
 // A lane's 16 states of a unit, in the caller's layout (units, E, N).
 __device__ __forceinline__ void load_states(const float* s, const ScanParams& p, int64_t unit, int64_t e, int n0,
@@ -185,5 +170,6 @@ __device__ __forceinline__ float time_step(const ScanParams& p, float v) { retur
 
 hipError_t launch_scan_both(const ScanParams& p, bool bf16, hipStream_t stream);
 hipError_t launch_scan_pass(const ScanParams& p, hipStream_t stream);
+bool scan_fits(const ScanParams& p);   // the grids of the chunk and pass kernels
 
 }  // namespace ssd

@@ -27,18 +27,18 @@ enum Mode { kOutput, kOutputReady, kStates, kBoth };
 
 // kOutput: y and final states.  kStates: each chunk's state from zero (from the
 // initial state in the first one), its sum of dt, and the time steps themselves,
-// which kOutputReady then takes as they are (13 instructions of 128 a token).  For the gradients, kBoth: that,
-// and the gradient of the state entering each chunk from the chunk's own outputs,
-// sum_t exp(A sum_{s <= t} dt_s) dy~_t C_t (walked forwards too, the product of the
-// decays so far kept: one exp2 serves both), and in front of every tile of kBwdTile
-// tokens the state, from zero as it is, and the sum of dt since the chunk's start.
+// which kOutputReady then takes as they are (97 instructions a token where kOutput
+// has 111).  For the gradients, kBoth: the states, the gradient of the state entering
+// each chunk from the chunk's own outputs, sum_t exp(A sum_{s <= t} dt_s) dy~_t C_t
+// (walked forwards too, the product of the decays so far kept: one exp2 serves
+// both), and in front of every tile of kBwdTile tokens the state, from zero as it
+// is, and the sum of dt since the chunk's start.
 // Workgroup: a wavefront per 16 states, at most THREADS / 64 of them (the bound
 // says how many registers a lane may have).
 //
 // A tile is kTok tokens; the next one's are loaded, and its B and C a token ahead,
-// before they are needed.  With several wavefronts their shares
-// of y meet in shared memory, and wavefront k finishes every token u = k, k +
-// slices, ..
+// before they are needed.  With several wavefronts their shares of y meet in shared
+// memory, and wavefront k finishes every token u = k, k + slices, ..
 template <typename T, bool PACKED, bool GATE, Mode MODE, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_scan_chunk(ScanParams p)
 {
@@ -345,7 +345,7 @@ hipError_t step(const ScanParams& p, hipStream_t stream)
         ++log2seg;
     }
     const int64_t grid = ((p.b + ROWS - 1) / ROWS * p.E * seg + 255) / 256;
-    if (grid > kMaxGrid) return hipErrorInvalidConfiguration;
+    if (!fits(grid, 256)) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL((k_scan_step<T, ROWS>), dim3(static_cast<unsigned>(grid)), dim3(256), 0, stream, p, seg, log2seg);
     return hipGetLastError();
 }
@@ -356,7 +356,6 @@ hipError_t chunk(const ScanParams& p, hipStream_t stream)
     const int64_t units = p.b * p.S * p.G * scan_tiles(p.E, p.G);
     const int slices = static_cast<int>(p.N / kSlice);
     const size_t lds = (MODE == kOutput || MODE == kOutputReady) && slices > 1 ? 2 * kTok * slices * 64 * sizeof(float) : 0;
-    if (units > kMaxGrid) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL((k_scan_chunk<T, PACKED, GATE, MODE, THREADS>), dim3(static_cast<unsigned>(units)), dim3(64 * slices),
                        lds, stream, p);
     return hipGetLastError();
@@ -394,7 +393,6 @@ hipError_t launch_scan_both(const ScanParams& p, bool bf16, hipStream_t stream)
 hipError_t launch_scan_pass(const ScanParams& p, hipStream_t stream)
 {
     const int64_t grid = (p.b * p.N * p.E + 255) / 256;
-    if (grid > kMaxGrid) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL(k_scan_pass, dim3(static_cast<unsigned>(grid)), dim3(256), 0, stream, p);
     return hipGetLastError();
 }
@@ -447,8 +445,14 @@ ScanPlan scan_plan(int64_t b, int64_t T, int64_t E, int64_t N, int64_t G, bool b
     return w;
 }
 
+bool scan_fits(const ScanParams& p)
+{
+    return fits(p.b * p.S * p.G * scan_tiles(p.E, p.G), 4 * p.N) && fits((p.b * p.N * p.E + 255) / 256, 256);
+}
+
 hipError_t launch_scan_forward(const ScanParams& p, bool bf16, hipStream_t stream)
 {
+    if (!scan_fits(p)) return hipErrorInvalidConfiguration;
     if (p.S > 1) {
         hipError_t err = bf16 ? chunks<uint16_t, kStates>(p, stream) : chunks<float, kStates>(p, stream);
         if (err == hipSuccess) err = launch_scan_pass(p, stream);

@@ -161,12 +161,14 @@ __device__ __forceinline__ const R& half(const R& lo, const R& hi)
         return hi;
 }
 
-// A tile of k_scan_grad (FULL: all its kBwdTile tokens are real); adds to the
-// channel's sums of dD and ddt_bias.
-template <typename T, bool PACKED, bool GATE, bool FULL>
+// A tile of k_scan_grad (FULL: all its kBwdTile tokens are real; PARTIAL: a group's
+// last channel tile may have lanes without a channel, which add zeros to the sums
+// over channels); adds to the channel's sums of dD and ddt_bias.
+template <typename T, bool PACKED, bool GATE, bool PARTIAL, bool FULL>
 __device__ __forceinline__ void grad_tile(const ScanParams& p, const ScanWork& w, int64_t tile, float* gs, float* as,
                                           float* extra, float bias, float D, float& sumD, float& sumBias)
 {
+    const bool live = !PARTIAL || w.live;
     const int lane = threadIdx.x, N = static_cast<int>(p.N);
     const int64_t t0 = tile * kBwdTile, out = (w.row * p.T + t0) * p.E + w.e0;
     const int64_t tiles = (p.T + kBwdTile - 1) / kBwdTile;
@@ -200,7 +202,7 @@ __device__ __forceinline__ void grad_tile(const ScanParams& p, const ScanWork& w
 #pragma unroll
         for (int u = 0; u < kBwdTile; ++u) {
             xv[u] = widen(xr[u]);
-            const float v = widen(dr[u]) + bias, dyv = w.live ? widen(yr[u]) : 0.f;
+            const float v = widen(dr[u]) + bias, dyv = live ? widen(yr[u]) : 0.f;
             d[u] = v;
             if (p.softplus) {
                 const float e = exp_neg(fabsf(v));
@@ -309,10 +311,10 @@ __device__ __forceinline__ void grad_tile(const ScanParams& p, const ScanWork& w
             const int64_t unit = scan_unit<PACKED>(p, w.row, t0 + u);
 #pragma unroll
             for (int n = 0; n < kQuad; ++n)
-                g[n] = p.dfin && w.live ? p.dfin[(unit * p.E + w.e) * p.N + q + n] : 0.f;
+                g[n] = p.dfin && live ? p.dfin[(unit * p.E + w.e) * p.N + q + n] : 0.f;
         };
         const auto arrive = [&](int u) {
-            if (!p.dinit || !w.live) return;
+            if (!p.dinit || !live) return;
             const int64_t unit = scan_unit<PACKED>(p, w.row, t0 + u);
 #pragma unroll
             for (int n = 0; n < kQuad; ++n) p.dinit[(unit * p.E + w.e) * p.N + q + n] = g[n];
@@ -352,7 +354,8 @@ __device__ __forceinline__ void grad_tile(const ScanParams& p, const ScanWork& w
                 if (PACKED && (starts >> u & 1)) arrive(u);
             }
             each<0, 2 * kQuad>([&](auto n) {
-                sums.template put<first + decltype(n)::value>(products[decltype(n)::value], lane);
+                constexpr int k = decltype(n)::value;
+                sums.template put<first + k>(live ? products[k] : 0.f, lane);
             });
         });
         if (!PACKED && t0 == 0) arrive(0);
@@ -377,7 +380,7 @@ __device__ __forceinline__ void grad_tile(const ScanParams& p, const ScanWork& w
             if (p.softplus) dd *= slope[u * 64];
             sumD = fmaf(dyg[u], xv[u], sumD);
             sumBias += dd;
-            if (w.live) {
+            if (live) {
                 const unsigned off = lane_offset<T>(w.lane);
                 dx.put(off, narrow<T>(fmaf(d[u], du[u], D * dyg[u])));
                 ddt.put(off, narrow<T>(dd));
@@ -393,12 +396,13 @@ __device__ __forceinline__ void grad_tile(const ScanParams& p, const ScanWork& w
 // One wavefront: 64 channels of one chunk, its tiles from the last to the first.
 // Shared memory: the states' running gradients g and sums of dA, [2][N][64], and two
 // values of each of the tile's tokens, [2][kBwdTile][64].
-template <typename T, bool PACKED, bool GATE>
+template <typename T, bool PACKED, bool GATE, bool PARTIAL>
 __global__ __launch_bounds__(64, 2) void k_scan_grad(ScanParams p)
 {
     extern __shared__ float shared[];
     const int lane = threadIdx.x, N = static_cast<int>(p.N);
     const ScanWork w = scan_work(p, blockIdx.x);
+    const bool live = !PARTIAL || w.live;
     float* const gs = shared + lane;
     float* const as = shared + N * 64 + lane;
     float* const extra = shared + 2 * N * 64;
@@ -406,17 +410,17 @@ __global__ __launch_bounds__(64, 2) void k_scan_grad(ScanParams p)
     float sumD = 0.f, sumBias = 0.f;
     const float* from = p.rstates + (w.row * p.S + w.chunk) * p.N * p.E + w.e;
     for (int n = 0; n < N; ++n) {
-        gs[n * 64] = w.live && p.S > 1 ? from[n * p.E] : 0.f;
+        gs[n * 64] = live && p.S > 1 ? from[n * p.E] : 0.f;
         as[n * 64] = 0.f;
     }
     int64_t tile = (w.t1 - 1) / kBwdTile;
     if (w.t1 - tile * kBwdTile < kBwdTile) {
-        grad_tile<T, PACKED, GATE, false>(p, w, tile, gs, as, extra, bias, D, sumD, sumBias);
+        grad_tile<T, PACKED, GATE, PARTIAL, false>(p, w, tile, gs, as, extra, bias, D, sumD, sumBias);
         --tile;
     }
     for (; tile * kBwdTile >= w.t0; --tile)
-        grad_tile<T, PACKED, GATE, true>(p, w, tile, gs, as, extra, bias, D, sumD, sumBias);
-    if (!w.live) return;
+        grad_tile<T, PACKED, GATE, PARTIAL, true>(p, w, tile, gs, as, extra, bias, D, sumD, sumBias);
+    if (!live) return;
     const int64_t rc = w.row * p.S + w.chunk;
     for (int n = 0; n < N; ++n) p.pA[(rc * p.N + n) * p.E + w.e] = as[n * 64];
     p.pD[rc * 2 * p.E + w.e] = sumD;
@@ -454,17 +458,25 @@ __global__ __launch_bounds__(256) void k_scan_sum_bc(ScanParams p, int64_t block
     to[tg * p.N + (n < p.N ? n : n - p.N)] = narrow<T>(v);
 }
 
-template <typename T, bool PACKED, bool GATE>
+template <typename T, bool PACKED, bool GATE, bool PARTIAL>
 hipError_t grad(const ScanParams& p, int64_t units, hipStream_t stream)
 {
     const size_t lds = 2 * static_cast<size_t>(p.N + kBwdTile) * 64 * sizeof(float);
     if (lds > 65536) {   // (N > 120) beyond the default limit
-        const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_scan_grad<T, PACKED, GATE>),
+        const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_scan_grad<T, PACKED, GATE, PARTIAL>),
                                                    hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));
         if (err != hipSuccess) return err;
     }
-    hipLaunchKernelGGL((k_scan_grad<T, PACKED, GATE>), dim3(static_cast<unsigned>(units)), dim3(64), lds, stream, p);
+    hipLaunchKernelGGL((k_scan_grad<T, PACKED, GATE, PARTIAL>), dim3(static_cast<unsigned>(units)), dim3(64), lds, stream, p);
     return hipGetLastError();
+}
+
+template <typename T, bool PACKED>
+hipError_t grads(const ScanParams& p, int64_t units, hipStream_t stream)
+{
+    const bool partial = p.E / p.G % 64 != 0;
+    if (p.z) return partial ? grad<T, PACKED, true, true>(p, units, stream) : grad<T, PACKED, true, false>(p, units, stream);
+    return partial ? grad<T, PACKED, false, true>(p, units, stream) : grad<T, PACKED, false, false>(p, units, stream);
 }
 
 template <typename T, bool PACKED>
@@ -473,15 +485,13 @@ hipError_t run(const ScanParams& p, hipStream_t stream)
     const int64_t units = p.b * p.S * p.G * scan_tiles(p.E, p.G);
     const int64_t sums = (p.N * p.E + 2 * p.E + kSumCols - 1) / kSumCols, bc = (p.b * p.T * p.G * 2 * p.N + 255) / 256;
     const int64_t pass = (p.b * p.N * p.E + 255) / 256;
-    if (units > kMaxGrid || sums > kMaxGrid || bc > kMaxGrid || pass > kMaxGrid) return hipErrorInvalidConfiguration;
+    if (!scan_fits(p) || !fits(sums, kSumLanes * kSumCols) || !fits(bc, 256)) return hipErrorInvalidConfiguration;
     if (hipError_t err = launch_scan_both(p, sizeof(T) == 2, stream); err != hipSuccess) return err;
     if (p.S > 1) {
         if (hipError_t err = launch_scan_pass(p, stream); err != hipSuccess) return err;
         hipLaunchKernelGGL(k_scan_rev_pass, dim3(static_cast<unsigned>(pass)), dim3(256), 0, stream, p);
     }
-    if (hipError_t err = p.z ? grad<T, PACKED, true>(p, units, stream) : grad<T, PACKED, false>(p, units, stream);
-        err != hipSuccess)
-        return err;
+    if (hipError_t err = grads<T, PACKED>(p, units, stream); err != hipSuccess) return err;
     hipLaunchKernelGGL(k_scan_sum_params, dim3(static_cast<unsigned>(sums)), dim3(kSumLanes * kSumCols), 0, stream, p);
     hipLaunchKernelGGL((k_scan_sum_bc<T>), dim3(static_cast<unsigned>(bc)), dim3(256), 0, stream, p,
                        scan_tiles(p.E, p.G));

@@ -842,31 +842,37 @@ def _act_dtype(x) -> int:
 
 
 def _check(x, act=(), f32=(), whole=(), strided=()):
-    """Types and devices of a call's tensors, (name, tensor or None, shape)
+    """Types, devices and shapes of a call's tensors, (name, tensor or None, shape)
     each: ``act`` of x's type, ``f32`` float32, ``whole`` of any type; all of
     them contiguous but those of ``strided`` (of x's type too), which need a
     contiguous last dimension."""
     import torch
 
-    for name, t, shape in tuple(act) + tuple(strided):
-        if t is not None and t.dtype != x.dtype:
-            raise TypeError("%s must have x's dtype" % name)
+    on, kind, single = x.get_device(), x.dtype, torch.float32
+    for name, t, shape in act:
+        if t is not None and not (t.dtype is kind and t.get_device() == on and t.shape == shape and t.is_contiguous()):
+            _refuse(name, t, shape, on, kind, "x's dtype")
     for name, t, shape in f32:
-        if t is not None and t.dtype != torch.float32:
-            raise TypeError("%s must be float32" % name)
-    for name, t, shape in tuple(act) + tuple(f32) + tuple(whole) + tuple(strided):
-        if t is None:
-            continue
-        if t.device != x.device:
-            raise ValueError("%s must be on x's device" % name)
-        if tuple(t.shape) != tuple(shape):
-            raise ValueError("%s must have shape %s, not %s" % (name, tuple(shape), tuple(t.shape)))
-    for name, t, shape in tuple(act) + tuple(f32) + tuple(whole):
-        if t is not None and not t.is_contiguous():
-            raise ValueError("%s must be contiguous" % name)
+        if t is not None and not (t.dtype is single and t.get_device() == on and t.shape == shape and t.is_contiguous()):
+            _refuse(name, t, shape, on, single, "dtype float32")
+    for name, t, shape in whole:
+        if t is not None and not (t.get_device() == on and t.shape == shape and t.is_contiguous()):
+            _refuse(name, t, shape, on, t.dtype, "")
     for name, t, shape in strided:
-        if t is not None and t.shape[-1] > 1 and t.stride(-1) != 1:
-            raise ValueError("%s must be contiguous in its last dimension" % name)
+        if t is not None and not (t.dtype is kind and t.get_device() == on and t.shape == shape
+                                  and (t.stride(-1) == 1 or shape[-1] == 1)):
+            _refuse(name, t, shape, on, kind, "x's dtype", "contiguous in its last dimension")
+
+
+def _refuse(name, t, shape, on, kind, wanted, order="contiguous"):
+    """Says what is wrong with a tensor that ``_check`` does not take."""
+    if t.dtype is not kind:
+        raise TypeError("%s must have %s" % (name, wanted))
+    if t.get_device() != on:
+        raise ValueError("%s must be on x's device" % name)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError("%s must have shape %s, not %s" % (name, tuple(shape), tuple(t.shape)))
+    raise ValueError("%s must be %s" % (name, order))
 
 
 def _out(out, like_shape, dtype, device, name="out"):
@@ -913,12 +919,18 @@ def _sized(name, prob):
     return int(need.value)
 
 
+_Parts = ctypes.c_int64 * 3
+
+
 def _conv_problem(x, weight, split, silu, nseq, dtype):
     b, T, C = x.shape
-    split = (C,) if split is None else tuple(int(k) for k in split)
-    if not 1 <= len(split) <= 3 or min(split) < 1 or sum(split) != C:
-        raise ValueError("split must be 1 to 3 positive sizes that add up to %d channels" % C)
-    parts = (ctypes.c_int64 * 3)(*(split + (0,) * (3 - len(split))))
+    if split is None:
+        split = (C,)
+    else:
+        split = tuple(int(k) for k in split)
+        if not 1 <= len(split) <= 3 or min(split) < 1 or sum(split) != C:
+            raise ValueError("split must be 1 to 3 positive sizes that add up to %d channels" % C)
+    parts = _Parts(*split)
     return SsdConvProblem(b, T, C, weight.shape[1], nseq, x.stride(0), x.stride(1), len(split), parts, dtype,
                           int(bool(silu))), split
 
@@ -1014,7 +1026,7 @@ def conv_step(x, weight, state, bias=None, silu: bool = True, out=None):
     return y
 
 
-_NO_PARTS = (ctypes.c_int64 * 3)()
+_NO_PARTS = _Parts()
 
 
 def _check_conv_step(x, weight, state, bias):
@@ -1029,12 +1041,11 @@ def _check_conv_step(x, weight, state, bias):
 
 
 def _scan_problem(x, dt, B, C, z, softplus, nseq, dtype):
-    def strides(t):
-        return (t.stride(0), t.stride(1)) if t is not None else (0, 0)
-
     b, T, E = x.shape
-    return SsdScanProblem(b, T, E, B.shape[3], B.shape[2], nseq, *strides(x), *strides(dt), *strides(z), *strides(B),
-                          *strides(C), dtype, int(bool(softplus)))
+    G, N = B.shape[2:]
+    zs = z.stride() if z is not None else (0, 0)
+    return SsdScanProblem(b, T, E, N, G, nseq, *x.stride()[:2], *dt.stride()[:2], *zs[:2], *B.stride()[:2],
+                          *C.stride()[:2], dtype, 1 if softplus else 0)
 
 
 def _scan_checked(x, dt, A_log, B, C, D, z, dt_bias, initial_states, seq_idx, nseq, softplus, more_act=(), more_f32=()):
@@ -1099,8 +1110,8 @@ def scan_backward(x, dt, A_log, B, C, dy, D=None, z=None, dt_bias=None, dt_softp
     need = _sized("ssd_scan_backward_workspace_bytes", prob)
     workspace = _room(workspace, need, x.device)
 
-    def new(t, kind=None):
-        return torch.empty(t.shape, dtype=kind or t.dtype, device=t.device) if t is not None else None
+    def new(t):
+        return torch.empty(t.shape, dtype=t.dtype, device=t.device) if t is not None else None
 
     g = {"dx": new(x), "ddt": new(x), "dB": new(B), "dC": new(C), "dz": new(z), "dA_log": new(A_log), "dD": new(D),
          "ddt_bias": new(dt_bias),
