@@ -142,6 +142,39 @@ def test_an_infinite_sequence_stays_by_itself(T, starts):
         assert same(a[[0, 2]], c[[0, 2]])
 
 
+@pytest.mark.parametrize("E", [5, 64])
+def test_an_infinite_operand_makes_no_nan_of_its_own(E):
+    """One channel's input is infinite at one token: the sums over channels are
+    infinite where the definition's are, and a NaN only where they are."""
+    announce("scan: one infinite operand (%d channels)" % E)
+    i = inputs(1, 40, E, 16, 1, "f32", 1, gate=False, init=False)
+    i["x"][0, 11, E - 1] = float("inf")
+    dy = Draw(9)(1, 40, E)
+    g = ssd.scan_backward(**i, dy=dy)
+    names = {"softplus": True, "init": None, "spans": mixer.rows(1, 40),
+             **{k: i[k] for k in ("x", "dt", "A_log", "B", "C", "D", "z", "dt_bias")}}
+    want = mixer.scan_backward(**names, dy=dy, dfinal=None)
+    for k in ("dB", "dC"):
+        got = g[k].cpu()
+        assert torch.equal(torch.isnan(got), torch.isnan(want[k])) and torch.equal(torch.isinf(got), torch.isinf(want[k]))
+
+
+def test_strides_that_play_no_part():
+    """Strides over a single batch row or token may be anything."""
+    announce("scan, conv: strides over one row or token")
+    i = inputs(1, 9, 70, 16, 1, "bf16", 1)
+    want = ssd.scan_forward(**i)
+    odd = {**i, "B": i["B"].as_strided((1, 9, 1, 16), (7, 16, 16, 1)), "C": i["C"].as_strided((1, 9, 1, 16), (13, 16, 5, 1)),
+           "x": i["x"].as_strided((1, 9, 70), (1, 70, 1))}
+    assert same(ssd.scan_forward(**odd), want)
+    one = {k: v[:, :1] if k in ("x", "dt", "z", "B", "C") else v for k, v in i.items()}
+    want = ssd.scan_forward(**one)
+    odd = {**one, "B": one["B"].as_strided((1, 1, 1, 16), (7, 3, 1, 1)), "x": one["x"].as_strided((1, 1, 70), (3, 1 << 40, 1))}
+    assert same(ssd.scan_forward(**odd), want)
+    w = Draw(1)(70, 4)
+    assert same(ssd.conv_forward(odd["x"], w), ssd.conv_forward(one["x"], w))
+
+
 def test_small_and_large_steps():
     """dt over its whole range: softplus to float32's precision (2e-7 relative) where
     it is as small as e^v and where it is v, seen through one token."""
