@@ -5,14 +5,22 @@
 //     t = r w, m = max |t|:  q = round(t / m top),  scale = m rstd / top
 //     n = r rstd, g = dy w:  dr = rstd (g - n mean(g n)) + dresidual,  dw = sum dy n
 //
-// Bound by HBM: every tensor is read or written once.  `LANES` lanes share a row
-// and keep it in registers (NV vectors of 8 values a lane) between the row's
-// sums and the stores.  Where there are enough rows to fill the device a row is a
-// wavefront's (sums in registers, no barrier); fewer rows take a workgroup each.
+// Bound by HBM: every tensor is read or written once.  A row is a workgroup's, as
+// wide as the row is with 8 values a lane (up to 1,024 lanes, then 16 or 32 values),
+// and stays in registers between the row's sums and the stores.  A wavefront a row,
+// which needs no barrier, is slower or no faster in nearly every size: its 40 or 64
+// values a lane leave few wavefronts (y of 16,384 x 2,560 bf16 60 us, 69; of 16,384 x
+// 4,096 91, 156; with 8 values a lane 4,096 x 500 5.2, 4.8).
+//
+// Measured without a residual, 16,384 x 2,560 in bf16, repeated on the same tensors
+// (in part from the cache): y 60 us, e4m3 53, gradients 51.  From HBM, with a
+// float32 residual stream: 92 us (5.5 TB/s), e4m3 with a bf16 one 61, gradients 144.
 //
 // q needs no rstd: t / m is the same for a row however it is scaled, so the
 // rounding is of the exact quotient of two float32 products and does not depend
 // on the order of the row's sum.
+#include <type_traits>
+
 #include "ssd_internal.h"
 #include "ssd_ops.h"
 
@@ -21,39 +29,33 @@ namespace {
 
 constexpr int kV = 8;
 
-template <typename T>
-__device__ __forceinline__ void load8(const T* row, int64_t c, int64_t C, float (&v)[kV])
-{
-    if (c + kV <= C) {
-        const auto a = Pack<T, 4>::load(row + c), b = Pack<T, 4>::load(row + c + 4);
+// kV values of a row from column c on, as they lie in memory.  WHOLE: C is a
+// multiple of kV, and where c is behind the row's end its last values stand in, so
+// that no branch parts one load from the next (with the branches of the other case,
+// zeros behind the end, each load waits for the one before: gradients of 16,384 x
+// 2,560 bf16 51 us, of 16,384 x 2,561 62).
+template <typename T, bool WHOLE>
+struct Values {
+    static constexpr int kWide = sizeof(T) == 2 ? 8 : 4;
+    Pack<T, kWide> part[kV / kWide];
+    __device__ __forceinline__ float operator[](int e) const { return part[e / kWide][e % kWide]; }
+    __device__ __forceinline__ void load(const T* row, int c, int C)
+    {
+        if (WHOLE || c + kV <= C) {
+            if (WHOLE) c = c < C ? c : C - kV;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            v[e] = a[e];
-            v[4 + e] = b[e];
+            for (int k = 0; k < kV / kWide; ++k) part[k] = Pack<T, kWide>::load(row + c + k * kWide);
+            return;
         }
-        return;
+#pragma unroll
+        for (int e = 0; e < kV; ++e) part[e / kWide].v[e % kWide] = c + e < C ? row[c + e] : T{};
     }
-#pragma unroll
-    for (int e = 0; e < kV; ++e) v[e] = c + e < C ? widen(row[c + e]) : 0.f;
-}
+};
 
-template <>
-__device__ __forceinline__ void load8<uint16_t>(const uint16_t* row, int64_t c, int64_t C, float (&v)[kV])
+template <bool WHOLE, typename T>
+__device__ __forceinline__ void store8(T* row, int c, int C, const float (&v)[kV])
 {
-    if (c + kV <= C) {
-        const auto a = Pack<uint16_t, 8>::load(row + c);
-#pragma unroll
-        for (int e = 0; e < kV; ++e) v[e] = a[e];
-        return;
-    }
-#pragma unroll
-    for (int e = 0; e < kV; ++e) v[e] = c + e < C ? widen(row[c + e]) : 0.f;
-}
-
-template <typename T>
-__device__ __forceinline__ void store8(T* row, int64_t c, int64_t C, const float (&v)[kV])
-{
-    if (c + kV <= C) {
+    if (WHOLE || c + kV <= C) {
         constexpr int N = sizeof(T) == 2 ? 8 : 4;
 #pragma unroll
         for (int k = 0; k < kV; k += N) {
@@ -70,9 +72,10 @@ __device__ __forceinline__ void store8(T* row, int64_t c, int64_t C, const float
 }
 
 // Eight bytes, packed low to high.
-__device__ __forceinline__ void store8b(uint8_t* row, int64_t c, int64_t C, uint32_t lo, uint32_t hi)
+template <bool WHOLE>
+__device__ __forceinline__ void store8b(uint8_t* row, int c, int C, uint32_t lo, uint32_t hi)
 {
-    if (c + kV <= C) {
+    if (WHOLE || c + kV <= C) {
         typedef uint32_t u2 __attribute__((ext_vector_type(2), aligned(1)));
         *reinterpret_cast<u2*>(row + c) = u2{lo, hi};
         return;
@@ -88,13 +91,18 @@ __device__ __forceinline__ float dpp_max(float v)
     return fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, false)));
 }
 
-// Largest over the wavefront's lanes (of values >= 0).
-__device__ __forceinline__ float wave_max(float v)
+// Largest over 16 lanes, and over the wavefront's (of values >= 0).
+__device__ __forceinline__ float row_max16(float v)
 {
     v = dpp_max<0x128>(v);
     v = dpp_max<0x124>(v);
     v = dpp_max<0x122>(v);
-    v = dpp_max<0x121>(v);
+    return dpp_max<0x121>(v);
+}
+
+__device__ __forceinline__ float wave_max(float v)
+{
+    v = row_max16(v);
     uint32_t u = __float_as_uint(v);
     const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
     v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
@@ -103,102 +111,91 @@ __device__ __forceinline__ float wave_max(float v)
     return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
-// A row's sum and maximum over its LANES lanes.
-template <int LANES>
-__device__ __forceinline__ void row_reduce(float& sum, float& most)
+// The sums (or maxima) of a workgroup's wavefronts, one in every lane l % 16, joined.
+__device__ __forceinline__ float waves_sum(const float* s)
 {
-    sum = wave_sum(sum);
-    most = wave_max(most);
-    if constexpr (LANES > 64) {
-        constexpr int W = LANES / 64;
-        __shared__ float s[2][W];
-        const int wave = threadIdx.x >> 6;
-        if ((threadIdx.x & 63) == 0) {
-            s[0][wave] = sum;
-            s[1][wave] = most;
-        }
-        __syncthreads();
-        sum = 0.f;
-        most = 0.f;
-#pragma unroll
-        for (int k = 0; k < W; ++k) {
-            sum += s[0][k];
-            most = fmaxf(most, s[1][k]);
-        }
-    }
+    const int l = threadIdx.x & 15;
+    return row_sum16(l < static_cast<int>(blockDim.x >> 6) ? s[l] : 0.f);
 }
 
-// LANES lanes a row; workgroups of at least 256 threads (4 rows of one wavefront).
-template <int LANES>
-constexpr int kBlock = LANES > 256 ? LANES : 256;
-
-template <typename T, typename R, NormOut OUT, int LANES, int NV>
-__global__ __launch_bounds__(kBlock<LANES>) void k_add_norm(NormParams p)
+__device__ __forceinline__ float waves_max(const float* s)
 {
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * (kBlock<LANES> / LANES) + uniform(threadIdx.x / LANES);
-    if (row >= p.rows) return;   // (whole wavefronts; with a workgroup a row, never)
-    const int lane = threadIdx.x % LANES;
+    const int l = threadIdx.x & 15;
+    return row_max16(l < static_cast<int>(blockDim.x >> 6) ? s[l] : 0.f);
+}
+
+constexpr int kWidest = 1024;
+
+template <typename T, typename R, NormOut OUT, int NV, bool WHOLE>
+__global__ __launch_bounds__(kWidest) void k_add_norm(NormParams p)
+{
+    const int64_t row = blockIdx.x;
+    const int lane = threadIdx.x, lanes = blockDim.x, C = static_cast<int>(p.C);
     const T* x = static_cast<const T*>(p.x) + row * p.C;
     const R* res = p.res ? static_cast<const R*>(p.res) + row * p.C : nullptr;
+    Values<T, WHOLE> in[NV];
+    Values<R, WHOLE> more[NV] = {};
+    Values<float, WHOLE> weight[NV];
     float r[NV][kV], sum = 0.f, most = 0.f;
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        const int64_t c = (static_cast<int64_t>(k) * LANES + lane) * kV;
-        if (c < p.C) {
-            load8(x, c, p.C, r[k]);
-            if (res) {
-                float a[kV];
-                load8(res, c, p.C, a);
+    for (int k = 0; k < NV; ++k) in[k].load(x, (k * lanes + lane) * kV, C);
+    if (res)
 #pragma unroll
-                for (int e = 0; e < kV; ++e) r[k][e] += a[e];
-            }
-        } else {
+        for (int k = 0; k < NV; ++k) more[k].load(res, (k * lanes + lane) * kV, C);
+    if (p.weight)
 #pragma unroll
-            for (int e = 0; e < kV; ++e) r[k][e] = 0.f;
-        }
-    }
+        for (int k = 0; k < NV; ++k) weight[k].load(p.weight, (k * lanes + lane) * kV, C);
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int e = 0; e < kV; ++e) r[k][e] = res ? in[k][e] + more[k][e] : in[k][e];
     if (p.res_out) {
         R* out = static_cast<R*>(p.res_out) + row * p.C;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            const int64_t c = (static_cast<int64_t>(k) * LANES + lane) * kV;
-            if (c < p.C) store8(out, c, p.C, r[k]);
+            const int c = (k * lanes + lane) * kV;
+            if (c < C) store8<WHOLE>(out, c, C, r[k]);
         }
     }
     // r becomes t = r w
-    bool odd = false;   // some t is infinite or a NaN
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-        const int64_t c = (static_cast<int64_t>(k) * LANES + lane) * kV;
-        float w[kV];
-        if (p.weight && c < p.C) {
-            load8(p.weight, c, p.C, w);
-        } else {
-#pragma unroll
-            for (int e = 0; e < kV; ++e) w[e] = 1.f;
-        }
+        float squares = 0.f, high = 0.f;
+        bool odd = false;   // some t is infinite or a NaN
 #pragma unroll
         for (int e = 0; e < kV; ++e) {
-            sum = fmaf(r[k][e], r[k][e], sum);
-            r[k][e] *= w[e];
+            squares = fmaf(r[k][e], r[k][e], squares);
+            if (p.weight) r[k][e] *= weight[k][e];
             if (OUT != kNormSame) {
                 const float m = fabsf(r[k][e]);
                 odd |= !(m < INFINITY);
-                most = fmaxf(most, m);
+                high = fmaxf(high, m);
             }
         }
+        if (odd) high = INFINITY;
+        const bool live = (k * lanes + lane) * kV < C;
+        sum += live ? squares : 0.f;
+        most = fmaxf(most, live ? high : 0.f);
     }
-    if (odd) most = INFINITY;
-    row_reduce<LANES>(sum, most);
+    sum = wave_sum(sum);
+    if (OUT != kNormSame) most = wave_max(most);
+    __shared__ float s[2][kWidest / 64];
+    if ((lane & 63) == 0) {
+        s[0][lane >> 6] = sum;
+        s[1][lane >> 6] = most;
+    }
+    __syncthreads();
+    sum = waves_sum(s[0]);
+    if (OUT != kNormSame) most = waves_max(s[1]);
     const float rstd = 1.f / sqrtf(sum / static_cast<float>(p.C) + p.eps);
     if constexpr (OUT == kNormSame) {
         T* y = static_cast<T*>(p.y) + row * p.C;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            const int64_t c = (static_cast<int64_t>(k) * LANES + lane) * kV;
+            const int c = (k * lanes + lane) * kV;
 #pragma unroll
             for (int e = 0; e < kV; ++e) r[k][e] *= rstd;
-            if (c < p.C) store8(y, c, p.C, r[k]);
+            if (c < C) store8<WHOLE>(y, c, C, r[k]);
         }
     } else {
         constexpr float kTop = OUT == kNormI8 ? 127.f : 448.f;
@@ -208,8 +205,8 @@ __global__ __launch_bounds__(kBlock<LANES>) void k_add_norm(NormParams p)
         const bool none = bad || most == 0.f;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            const int64_t c = (static_cast<int64_t>(k) * LANES + lane) * kV;
-            if (c >= p.C) continue;
+            const int c = (k * lanes + lane) * kV;
+            if (c >= C) continue;
             uint32_t out[2] = {0, 0};
             if (!none) {
                 float v[kV];
@@ -227,107 +224,115 @@ __global__ __launch_bounds__(kBlock<LANES>) void k_add_norm(NormParams p)
                     }
                 }
             }
-            store8b(q, c, p.C, out[0], out[1]);
+            store8b<WHOLE>(q, c, C, out[0], out[1]);
         }
     }
 }
 
-// Gradients: a wavefront (or workgroup) takes every `step`-th row, with its
-// columns' sums of dweight in registers, one partial row of the workspace each.
-template <typename T, typename R, int LANES, int NV>
-__global__ __launch_bounds__(kBlock<LANES>) void k_add_norm_backward(NormParams p, int64_t step)
+// c, made where it is used: the compiler would keep the addresses of all of a row's
+// vectors in registers from one row to the next.
+__device__ __forceinline__ int here(int c)
 {
-    const int64_t first = static_cast<int64_t>(blockIdx.x) * (kBlock<LANES> / LANES) + uniform(threadIdx.x / LANES);
-    const int lane = threadIdx.x % LANES;
-    float dw[NV][kV];
-#pragma unroll
-    for (int k = 0; k < NV; ++k)
-#pragma unroll
-        for (int e = 0; e < kV; ++e) dw[k][e] = 0.f;
+    asm volatile("" : "+v"(c));
+    return c;
+}
+
+// Eight channels' operands of the gradients.
+template <typename T, typename R, bool WHOLE>
+struct GradValues {
+    Values<R, WHOLE> r, d;
+    Values<T, WHOLE> g;
+    __device__ __forceinline__ void load(const NormParams& p, int64_t row, int c)
+    {
+        const int C = static_cast<int>(p.C);
+        r.load(static_cast<const R*>(p.res) + row * p.C, c, C);
+        g.load(static_cast<const T*>(p.x) + row * p.C, c, C);
+        if (p.dres) d.load(static_cast<const R*>(p.dres) + row * p.C, c, C);
+    }
+};
+
+// Gradients: a workgroup takes every `step`-th row, with its columns' sums of
+// dweight in registers, one partial row of the workspace each.  With 8 channels a
+// lane the weights stay in registers too, and the next row is loaded before the
+// present one's sums are joined; a wider row has no registers for that and is read
+// once more, from the cache, after its sums (16,384 x 20,000 bf16 637 us, kept in
+// registers, which spill, 1,590).
+template <typename T, typename R, int NV, bool WHOLE>
+__global__ __launch_bounds__(kWidest) void k_add_norm_backward(NormParams p, int64_t step)
+{
+    constexpr bool kAhead = NV == 1;
+    const int64_t first = blockIdx.x;   // < step <= rows
+    const int lane = threadIdx.x, lanes = blockDim.x, C = static_cast<int>(p.C);
+    float dw[NV][kV] = {};
+    GradValues<T, R, WHOLE> now, next;
+    Values<float, WHOLE> w;
+    if constexpr (kAhead) {
+        next.load(p, first, lane * kV);
+        if (p.weight) w.load(p.weight, lane * kV, C);
+    }
+    int turn = 0;
     for (int64_t row = first; row < p.rows; row += step) {
-        const T* dy = static_cast<const T*>(p.x) + row * p.C;
-        const R* rp = static_cast<const R*>(p.res) + row * p.C;
-        float r[NV][kV], g[NV][kV], ss = 0.f, gr = 0.f;
+        float ss = 0.f, gr = 0.f;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            const int64_t c = (static_cast<int64_t>(k) * LANES + lane) * kV;
-            if (c < p.C) {
-                load8(rp, c, p.C, r[k]);
-                load8(dy, c, p.C, g[k]);
+            if constexpr (kAhead) {
+                now = next;
+                if (row + step < p.rows) next.load(p, row + step, lane * kV);
             } else {
-#pragma unroll
-                for (int e = 0; e < kV; ++e) r[k][e] = g[k][e] = 0.f;
+                const int c = here((k * lanes + lane) * kV);
+                now.load(p, row, c);
+                if (p.weight) w.load(p.weight, c, C);
             }
-        }
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            const int64_t c = (static_cast<int64_t>(k) * LANES + lane) * kV;
-            float w[kV];
-            if (p.weight && c < p.C) {
-                load8(p.weight, c, p.C, w);
-            } else {
-#pragma unroll
-                for (int e = 0; e < kV; ++e) w[e] = 1.f;
-            }
+            float squares = 0.f, products = 0.f;
 #pragma unroll
             for (int e = 0; e < kV; ++e) {
-                ss = fmaf(r[k][e], r[k][e], ss);
-                gr = fmaf(g[k][e] * w[e], r[k][e], gr);
+                const float r = now.r[e], g = now.g[e];
+                squares = fmaf(r, r, squares);
+                products = fmaf(p.weight ? g * w[e] : g, r, products);
             }
+            const bool live = (k * lanes + lane) * kV < C;
+            ss += live ? squares : 0.f;
+            gr += live ? products : 0.f;
         }
         ss = wave_sum(ss);
         gr = wave_sum(gr);
-        if constexpr (LANES > 64) {
-            constexpr int W = LANES / 64;
-            __shared__ float s[2][2][W];   // alternating, so that one barrier a row is enough
-            const int wave = threadIdx.x >> 6, turn = static_cast<int>((row - first) / step) & 1;
-            if ((threadIdx.x & 63) == 0) {
-                s[turn][0][wave] = ss;
-                s[turn][1][wave] = gr;
-            }
-            __syncthreads();
-            ss = gr = 0.f;
-#pragma unroll
-            for (int k = 0; k < W; ++k) {
-                ss += s[turn][0][k];
-                gr += s[turn][1][k];
-            }
+        __shared__ float s[2][2][kWidest / 64];   // alternating, so that one barrier a row is enough
+        if ((lane & 63) == 0) {
+            s[turn][0][lane >> 6] = ss;
+            s[turn][1][lane >> 6] = gr;
         }
+        __syncthreads();
+        ss = waves_sum(s[turn][0]);
+        gr = waves_sum(s[turn][1]);
+        turn ^= 1;
         const float n = static_cast<float>(p.C);
         const float rstd = 1.f / sqrtf(ss / n + p.eps);
         const float back = gr * rstd * rstd / n;   // mean(g n) rstd
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            const int64_t c = (static_cast<int64_t>(k) * LANES + lane) * kV;
-            if (c >= p.C) continue;
-            float w[kV], d[kV];
-            if (p.weight) {
-                load8(p.weight, c, p.C, w);
-            } else {
-#pragma unroll
-                for (int e = 0; e < kV; ++e) w[e] = 1.f;
+            const int c = kAhead ? lane * kV : here((k * lanes + lane) * kV);
+            if constexpr (!kAhead) {
+                now.load(p, row, c);
+                if (p.weight) w.load(p.weight, c, C);
             }
-            if (p.dres) {
-                load8(static_cast<const R*>(p.dres) + row * p.C, c, p.C, d);
-            } else {
-#pragma unroll
-                for (int e = 0; e < kV; ++e) d[e] = 0.f;
-            }
+            float out[kV];
 #pragma unroll
             for (int e = 0; e < kV; ++e) {
-                dw[k][e] = fmaf(g[k][e], r[k][e] * rstd, dw[k][e]);
-                d[e] = fmaf(rstd, fmaf(g[k][e], w[e], -r[k][e] * back), d[e]);
+                const float r = now.r[e], g = now.g[e], d = p.dres ? now.d[e] : 0.f;
+                dw[k][e] = fmaf(g, r * rstd, dw[k][e]);
+                out[e] = fmaf(rstd, (p.weight ? g * w[e] : g) - r * back, d);
             }
-            if (p.y) store8(static_cast<T*>(p.y) + row * p.C, c, p.C, d);
-            if (p.res_out) store8(static_cast<R*>(p.res_out) + row * p.C, c, p.C, d);
+            if (c >= C) continue;
+            if (p.y) store8<WHOLE>(static_cast<T*>(p.y) + row * p.C, c, C, out);
+            if (p.res_out) store8<WHOLE>(static_cast<R*>(p.res_out) + row * p.C, c, C, out);
         }
     }
-    if (p.partial && first < step) {
+    if (p.partial) {
         float* out = p.partial + first * p.C;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            const int64_t c = (static_cast<int64_t>(k) * LANES + lane) * kV;
-            if (c < p.C) store8(out, c, p.C, dw[k]);
+            const int c = (k * lanes + lane) * kV;
+            if (c < C) store8<WHOLE>(out, c, C, dw[k]);
         }
     }
 }
@@ -339,87 +344,76 @@ __global__ __launch_bounds__(kSumLanes * kSumCols) void k_norm_dw(const float* p
     if (threadIdx.x < kSumCols && c < C) dw[c] = v;
 }
 
-// Lanes a row: a wavefront where rows are many and short enough for its
-// registers, else a workgroup of 256 or (beyond 16,384 channels) 1,024.
-int row_lanes(int64_t rows, int64_t C)
+// Vectors a lane: one, as long as a workgroup is wide enough for the row.
+int vectors(int64_t C) { return C <= kWidest * kV ? 1 : C <= 2 * kWidest * kV ? 2 : 4; }
+
+int row_threads(int64_t C)
 {
-    if (C <= 64 * 8 * kV && rows >= 1024) return 64;
-    return C <= 256 * 8 * kV ? 256 : 1024;
+    const int64_t per = vectors(C) * kV * 64;
+    return static_cast<int>((C + per - 1) / per) * 64;
 }
 
-template <typename T, typename R, NormOut OUT, int LANES, int NV>
+template <typename T, typename R, NormOut OUT, int NV, bool WHOLE>
 hipError_t forward(const NormParams& p, hipStream_t stream)
 {
-    constexpr int64_t per = kBlock<LANES> / LANES;
-    const int64_t grid = (p.rows + per - 1) / per;
-    if (!fits(grid, kBlock<LANES>)) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL((k_add_norm<T, R, OUT, LANES, NV>), dim3(static_cast<unsigned>(grid)), dim3(kBlock<LANES>), 0,
-                       stream, p);
+    const int threads = row_threads(p.C);
+    if (!fits(p.rows, threads)) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL((k_add_norm<T, R, OUT, NV, WHOLE>), dim3(static_cast<unsigned>(p.rows)), dim3(threads), 0, stream, p);
     return hipGetLastError();
 }
 
-template <typename T, typename R, int LANES, int NV>
+template <typename T, typename R, int NV, bool WHOLE>
 hipError_t backward(const NormParams& p, hipStream_t stream)
 {
-    constexpr int64_t per = kBlock<LANES> / LANES;
-    const int64_t partials = norm_bwd_partials(p.rows, p.C);   // a multiple of `per`
-    hipLaunchKernelGGL((k_add_norm_backward<T, R, LANES, NV>), dim3(static_cast<unsigned>(partials / per)),
-                       dim3(kBlock<LANES>), 0, stream, p, partials);
+    const int64_t partials = norm_bwd_partials(p.rows, p.C);
+    hipLaunchKernelGGL((k_add_norm_backward<T, R, NV, WHOLE>), dim3(static_cast<unsigned>(partials)), dim3(row_threads(p.C)),
+                       0, stream, p, partials);
     return hipGetLastError();
 }
 
-template <int L, int V>
-struct Row {
-    static constexpr int lanes = L, vectors = V;
-};
-
-// f of the row's lanes and of the vectors that a lane holds.
+// f of the vectors that a lane holds and of whether C is a multiple of theirs.
 template <typename F>
 hipError_t by_row(const NormParams& p, F f)
 {
-    const int lanes = row_lanes(p.rows, p.C);
-    const int64_t per = static_cast<int64_t>(lanes) * kV, n = (p.C + per - 1) / per;
-    if (lanes == 1024) return n <= 3 ? f(Row<1024, 3>{}) : f(Row<1024, 4>{});
-    const auto with = [&](auto l) {
-        constexpr int L = decltype(l)::lanes;
-        if (n <= 1) return f(Row<L, 1>{});
-        if (n <= 2) return f(Row<L, 2>{});
-        if (n <= 3) return f(Row<L, 3>{});
-        if (n <= 5) return f(Row<L, 5>{});
-        return f(Row<L, 8>{});
+    const auto with = [&](auto whole) {
+        const int n = vectors(p.C);
+        return n == 1   ? f(std::integral_constant<int, 1>{}, whole)
+               : n == 2 ? f(std::integral_constant<int, 2>{}, whole)
+                        : f(std::integral_constant<int, 4>{}, whole);
     };
-    return lanes == 64 ? with(Row<64, 1>{}) : with(Row<256, 1>{});
+    return p.C % kV == 0 ? with(std::true_type{}) : with(std::false_type{});
 }
 
 template <typename T, typename R>
 hipError_t by_out(const NormParams& p, NormOut out, hipStream_t stream)
 {
-    return by_row(p, [&](auto row) {
-        constexpr int L = decltype(row)::lanes, V = decltype(row)::vectors;
-        if (out == kNormSame) return forward<T, R, kNormSame, L, V>(p, stream);
-        if (out == kNormI8) return forward<T, R, kNormI8, L, V>(p, stream);
-        return forward<T, R, kNormE4M3, L, V>(p, stream);
+    return by_row(p, [&](auto n, auto whole) {
+        constexpr int V = decltype(n)::value;
+        constexpr bool W = decltype(whole)::value;
+        if (out == kNormSame) return forward<T, R, kNormSame, V, W>(p, stream);
+        if (out == kNormI8) return forward<T, R, kNormI8, V, W>(p, stream);
+        return forward<T, R, kNormE4M3, V, W>(p, stream);
     });
 }
 
 template <typename T, typename R>
 hipError_t grads(const NormParams& p, hipStream_t stream)
 {
-    return by_row(p, [&](auto row) {
-        return backward<T, R, decltype(row)::lanes, decltype(row)::vectors>(p, stream);
+    return by_row(p, [&](auto n, auto whole) {
+        return backward<T, R, decltype(n)::value, decltype(whole)::value>(p, stream);
     });
 }
 
 }  // namespace
 
-// Wavefronts (or workgroups) of the gradient kernel: eight wavefronts a compute
-// unit; more would only write more partial rows of dweight.
+// Workgroups of the gradient kernel: 4,096 wavefronts, four a SIMD (16,384 x 4,096
+// bf16 79 us, 8,192 wavefronts 94; 16,384 x 8,192 150, 2,048 wavefronts 235), and at
+// least two rows each: a partial row of dweight for every row costs more to add up
+// than it saves (512 x 4,096 10.1 us, one row each 13.9).
 int64_t norm_bwd_partials(int64_t rows, int64_t C)
 {
-    const int lanes = row_lanes(rows, C);
-    const int64_t most = lanes == 64 ? 2048 : lanes == 256 ? 512 : 256, per = lanes == 64 ? 4 : 1;
-    const int64_t n = rows < most ? rows : most;
-    return (n + per - 1) / per * per;
+    const int64_t most = 4096 / (row_threads(C) / 64), n = (rows + 1) / 2;
+    return n < most ? n : most;
 }
 
 hipError_t launch_add_norm(const NormParams& p, bool bf16, bool res_bf16, NormOut out, hipStream_t stream)
