@@ -129,7 +129,8 @@ constexpr int kWidest = 1024;
 template <typename T, typename R, NormOut OUT, int NV, bool WHOLE>
 __global__ __launch_bounds__(kWidest) void k_add_norm(NormParams p)
 {
-    const int64_t row = blockIdx.x;
+    const int64_t row = static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x;
+    if (row >= p.rows) return;   // (whole workgroups)
     const int lane = threadIdx.x, lanes = blockDim.x, C = static_cast<int>(p.C);
     const T* x = static_cast<const T*>(p.x) + row * p.C;
     const R* res = p.res ? static_cast<const R*>(p.res) + row * p.C : nullptr;
@@ -356,9 +357,12 @@ int row_threads(int64_t C)
 template <typename T, typename R, NormOut OUT, int NV, bool WHOLE>
 hipError_t forward(const NormParams& p, hipStream_t stream)
 {
+    // a dimension of a launch has 32 bits of threads; the rows go on in the second (of
+    // the most elements that a tensor may have, 512 times)
     const int threads = row_threads(p.C);
-    if (!fits(p.rows, threads)) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL((k_add_norm<T, R, OUT, NV, WHOLE>), dim3(static_cast<unsigned>(p.rows)), dim3(threads), 0, stream, p);
+    const int64_t most = 0xffffffffLL / threads, x = p.rows < most ? p.rows : most, y = (p.rows + x - 1) / x;
+    hipLaunchKernelGGL((k_add_norm<T, R, OUT, NV, WHOLE>), dim3(static_cast<unsigned>(x), static_cast<unsigned>(y)),
+                       dim3(threads), 0, stream, p);
     return hipGetLastError();
 }
 

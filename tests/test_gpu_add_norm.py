@@ -166,3 +166,18 @@ def test_streams_and_capture():
         streams_and_graphs(lambda: ssd.add_norm(**i))
         streams_and_graphs(lambda: ssd.add_norm_q8(**i, dtype=torch.int8))
         streams_and_graphs(lambda: ssd.add_norm_backward(dy, i["residual"], i["weight"]))
+
+
+def test_more_rows_than_one_launch_dimension():
+    rows = (1 << 32) // 64 + 1000     # (a launch's dimension has 32 bits of threads, 64 a row)
+    announce("add_norm %d x 3" % rows)
+    x = torch.zeros(rows, 3, dtype=torch.bfloat16).cuda()
+    at = torch.cat([torch.arange(500), torch.arange((1 << 26) - 500, (1 << 26) + 500), torch.arange(rows - 500, rows)])
+    x[at.cuda()] = Draw(6)(len(at), 3, dtype=torch.bfloat16)
+    y, r = ssd.add_norm(x, torch.ones(3).cuda())
+    want, _ = mixer.add_norm(x[at.cuda()], torch.ones(3).cuda(), None, 1e-5)
+    check("y", y[at.cuda()], want)
+    assert int((y != 0).any(-1).sum()) <= len(at)
+    q, scale, _ = ssd.add_norm_q8(x, dtype=torch.int8)
+    some, s, _ = ssd.add_norm_q8(x[at.cuda()], dtype=torch.int8)
+    assert torch.equal(q[at.cuda()], some) and torch.equal(scale[at.cuda()], s)
