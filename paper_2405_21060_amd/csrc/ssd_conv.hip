@@ -8,8 +8,8 @@
 // Bound by HBM: x is read and y written once (gradients: x and dy read, dx
 // written).  A wavefront takes a strip of consecutive tokens of 64 x V channels
 // (V = 2 a lane; 4 and 8 hold more registers and leave fewer wavefronts: forward 4 x
-// 4,096 x 5,376 bf16 76 us, 84 and 92, gradients 1 x 32,768 x 6,144 283, 289 and
-// 333) and walks down the tokens with the W - 1 rows
+// 4,096 x 5,376 bf16 76 us, 84 and 92, gradients 1 x 32,768 x 6,144 in strips of 128
+// tokens 283, 289 and 333) and walks down the tokens with the W - 1 rows
 // before the present one in registers, so that a token's row is read once, and
 // the W - 1 rows in front of a strip once more.  Sequences of a packed row are the
 // wavefront's own control flow: at a sequence's first token the rows in
@@ -371,8 +371,8 @@ bool vectors(const ConvParams& p)
 
 // Tokens per strip: longer strips read fewer rows twice, shorter ones give more
 // wavefronts; the longest that leaves 4,096 (four a SIMD), else the shortest.  The
-// longest is 32 tokens (64: 80 us for the forward above) and 128 for the gradients
-// (64: 295 us), whose strips have a row of partial sums each.
+// longest is 32 tokens (64: 80 us for the forward above) and 256 for the gradients
+// (275 us; 128: 283, 64: 297), whose strips have a row of partial sums each.
 int64_t strip_tokens(int64_t b, int64_t T, int64_t tiles, int64_t longest, int64_t shortest)
 {
     int64_t R = longest;
@@ -435,7 +435,7 @@ hipError_t step_by_width(const ConvParams& p, hipStream_t stream)
 }  // namespace
 
 // (by the channels alone, not by the parts: the workspace depends on it)
-int64_t conv_bwd_strip(int64_t b, int64_t T, int64_t C) { return strip_tokens(b, T, (C + 127) / 128, 128, 16); }
+int64_t conv_bwd_strip(int64_t b, int64_t T, int64_t C) { return strip_tokens(b, T, (C + 127) / 128, 256, 16); }
 
 hipError_t launch_conv_forward(const ConvParams& p, bool bf16, hipStream_t stream)
 {
