@@ -4,6 +4,8 @@
 // Host validation: ssd_ops_api.cpp.
 #pragma once
 
+#include <cfloat>
+
 #include "ssd_device.h"
 
 namespace ssd {
@@ -125,11 +127,15 @@ __device__ __forceinline__ int64_t held(int32_t id, int64_t nseq)
 // exp(-v): 2^t (1 + r), t = -v log2(e) rounded and r what the rounding left over
 // (where 2^t alone is off by |v| 6e-8); relative error near 2e-7.  v is held to
 // +-104, beyond which the result is infinite or 0; a NaN counts as one of the two.
+// 2^t is infinite from v < -88.7 on and r of either sign, so r is taken of the largest
+// finite number there: infinity times an r of 0 or below would be a NaN, or make one.
+// LARGE: v may be that small (false: a v of 0 and more needs no such care).
+template <bool LARGE = true>
 __device__ __forceinline__ float exp_neg(float v)
 {
     v = __builtin_amdgcn_fmed3f(v, -104.f, 104.f);
     const float t = v * -kLog2e, e = __builtin_amdgcn_exp2f(t);
-    return fmaf(e, fmaf(t, -0.69314718f, -v), e);
+    return fmaf(LARGE ? fminf(e, FLT_MAX) : e, fmaf(t, -0.69314718f, -v), e);
 }
 
 __device__ __forceinline__ float sigmoid_hw(float v) { return __builtin_amdgcn_rcpf(1.f + exp_neg(v)); }
@@ -141,7 +147,7 @@ __device__ __forceinline__ float sigmoid_hw(float v) { return __builtin_amdgcn_r
 // time step is.  -infinity gives 0, a NaN a NaN.
 constexpr float kAtanh0 = 2.f, kAtanh1 = 0.666663229f, kAtanh2 = 0.400245965f, kAtanh3 = 0.279651582f, kAtanh4 = 0.281577796f;   // times 2
 
-__device__ __forceinline__ float softplus_hw(float v, float u)   // u = exp_neg(|v|)
+__device__ __forceinline__ float softplus_hw(float v, float u)   // u = exp_neg<false>(|v|)
 {
     const float s = u * __builtin_amdgcn_rcpf(2.f + u), q = s * s;
     float r = fmaf(q, kAtanh4, kAtanh3);
@@ -151,7 +157,7 @@ __device__ __forceinline__ float softplus_hw(float v, float u)   // u = exp_neg(
     return fmaf(s, r, __builtin_elementwise_maximum(v, 0.f));
 }
 
-__device__ __forceinline__ float softplus_hw(float v) { return softplus_hw(v, exp_neg(fabsf(v))); }
+__device__ __forceinline__ float softplus_hw(float v) { return softplus_hw(v, exp_neg<false>(fabsf(v))); }
 
 __device__ __forceinline__ float widen(float v) { return v; }
 __device__ __forceinline__ float widen(uint16_t v) { return __uint_as_float(static_cast<uint32_t>(v) << 16); }

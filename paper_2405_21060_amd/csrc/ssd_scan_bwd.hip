@@ -209,7 +209,7 @@ __device__ __forceinline__ void grad_tile(const ScanParams& p, const ScanWork& w
             const float v = widen(dr[u]) + bias, dyv = live ? widen(yr[u]) : 0.f;
             d[u] = v;
             if (p.softplus) {
-                const float e = exp_neg(fabsf(v));
+                const float e = exp_neg<false>(fabsf(v));
                 d[u] = softplus_hw(v, e);
                 slope[u * 64] = (v >= 0.f ? 1.f : e) * __builtin_amdgcn_rcpf(1.f + e);
             }

@@ -1,0 +1,85 @@
+"""The operators around the layer at the ends of their ranges on the GPU, against
+their float64 definitions: SiLU where its exponential overflows."""
+import pytest
+import torch
+
+from oracle import mixer
+from tests.mixer_harness import DTYPES, Draw, announce, check, same, seq_idx_of, ssd
+from tests.test_gpu_parity import _gpu  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def large_negatives(dtype):
+    """From -110 to -80: every bf16 value; 30,001 float32 ones, 0.001 apart."""
+    if dtype == "f32":
+        return torch.linspace(-110, -80, 30001)
+    return torch.arange(-110, -79.75, 0.25).bfloat16().unique()
+
+
+def lost(v):
+    """What v sigmoid(v) and its derivative may be off in all: a sigmoid below 2^-126 (v <
+    -87.3) may count as 0."""
+    v = v.double()
+    return torch.where(v < -87.3, v.abs() * 2.0 ** -126, 0.0)
+
+
+def near(name, got, want, roundings, apart):
+    """Every value within so many roundings of its own, and of its type's one."""
+    assert got.shape == want.shape
+    got = got.detach()
+    share = roundings * 2.0 ** -24 + (2.0 ** -8 if got.dtype == torch.bfloat16 else 0.0)
+    err = (got.cpu().double() - want).abs()
+    bad = ~(err <= share * want.abs() + apart)   # (a NaN is bad)
+    assert not bad.any(), "%s: %d of %d, first %s, want %s" % (name, bad.sum(), bad.numel(), got[bad.to(got.device)][0], want[bad][0])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_convolution_of_large_negative_sums(dtype):
+    """Exponentials, reciprocal, products: fewer than 16 roundings."""
+    v = large_negatives(dtype)
+    announce("conv: SiLU of %d values from -110 to -80 %s" % (len(v), dtype))
+    n, apart = len(v), lost(v)
+    x, w = v.cuda().view(1, 1, n), torch.zeros(n, 2).cuda()
+    w[:, 1] = 1.0
+    want, _ = mixer.conv_forward(x, w, None, True, None, mixer.rows(1, 1))
+    near("y", ssd.conv_forward(x, w)[0], want, 16, apart)
+    near("step", ssd.conv_step(x[0], w, torch.zeros(1, 1, n, dtype=x.dtype).cuda()), want[0], 16, apart)
+    dy, bias = torch.ones_like(x), torch.zeros(n).cuda()
+    g = ssd.conv_backward(x, w, dy, bias=bias)
+    want = mixer.conv_backward(x, w, bias, True, None, mixer.rows(1, 1), dy, None)
+    near("dx", g["dx"], want["dx"], 16, apart)
+    near("dbias", g["dbias"], want["dbias"], 16, apart)
+    near("dweight", g["dweight"], want["dweight"], 16, (apart * 110)[:, None])
+    assert torch.all(g["dinit"] == 0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_scan_gated_by_large_negatives(dtype):
+    """One token a channel, all operands 1: a value is a sum of at most 33 products with
+    one SiLU (or a derivative), no larger than 64 of it, all of one sign: 64 roundings;
+    the sums over channels are of 64 lanes and of up to 469 tiles."""
+    v = large_negatives(dtype)
+    announce("scan: a gate of %d values from -110 to -80 %s" % (len(v), dtype))
+    E, N, apart = len(v), 16, 64 * lost(v)
+    t = DTYPES[dtype]
+    one = torch.ones(1, 1, E, dtype=t).cuda()
+    i = {"x": one, "dt": one, "A_log": torch.zeros(E, N).cuda(), "B": torch.ones(1, 1, 1, N, dtype=t).cuda(),
+         "C": torch.ones(1, 1, 1, N, dtype=t).cuda(), "D": torch.ones(E).cuda(), "z": v.cuda().view(1, 1, E)}
+    state = torch.ones(1, E, N).cuda()
+    names = {**i, "dt_bias": None, "softplus": False, "init": state, "spans": mixer.rows(1, 1)}
+    want, want_f = mixer.scan_forward(**names)
+    y, f = ssd.scan_forward(**i, dt_softplus=False, initial_states=state)
+    near("y", y, want, 64, apart)
+    near("final", f, want_f, 64, 0.0)
+    g = ssd.scan_backward(**i, dy=one, dt_softplus=False, initial_states=state)
+    want_g = mixer.scan_backward(**names, dy=one, dfinal=None)
+    for k in ("dx", "ddt", "dz", "dD"):
+        near(k, g[k], want_g[k], 64, apart)
+    for k in ("dA_log", "dinit"):
+        near(k, g[k], want_g[k], 64, apart[:, None])
+    for k in ("dB", "dC"):
+        near(k, g[k], want_g[k], 64 + 64 + 469, apart.sum())
+    step = ssd.scan_step(one[:, 0], one[:, 0], i["A_log"], i["B"][:, 0], i["C"][:, 0], state, D=i["D"], z=i["z"][:, 0],
+                         dt_softplus=False)
+    near("step", step, want[0], 64, apart)
