@@ -242,7 +242,8 @@ __device__ __forceinline__ void grad_tile(const ScanParams& p, const ScanWork& w
     if (PACKED && reached)
         reached = !scan_starts<PACKED>(p, w.t0) &&
                   scalar_load(p.seq_idx + w.t0) == scalar_load(p.seq_idx + (t0 > w.t0 ? t0 - 1 : t0));
-    const float since = p.marksums[(w.row * tiles + tile) * p.E + w.e];
+    // (it runs on over sequences: where it is not of the tile's own one alone, it is not used)
+    const float since = reached ? p.marksums[(w.row * tiles + tile) * p.E + w.e] : 0.f;
     // the value that this lane gets of the 64: token, dB or dC, state
     const int place = static_cast<int>(__brev(static_cast<unsigned>(lane)) >> 26);
     const int tok = kBwdTile - 1 - place / (2 * kQuad);
@@ -281,7 +282,7 @@ __device__ __forceinline__ void grad_tile(const ScanParams& p, const ScanWork& w
         A2[3] = decay_rate(al.w);
 #pragma unroll
         for (int n = 0; n < kQuad; ++n) {
-            // (nothing reaches the tile: 0 times a decay)
+            // (nothing reaches the tile: 0 times 1)
             h[n] = fmaf(__builtin_amdgcn_exp2f(since * A2[n]), en[n], mn[n]);
             g[n] = gs[(q + n) * 64];
             dA[n] = as[(q + n) * 64];

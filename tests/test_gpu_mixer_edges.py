@@ -83,3 +83,61 @@ def test_scan_gated_by_large_negatives(dtype):
     step = ssd.scan_step(one[:, 0], one[:, 0], i["A_log"], i["B"][:, 0], i["C"][:, 0], state, D=i["D"], z=i["z"][:, 0],
                          dt_softplus=False)
     near("step", step, want[0], 64, apart)
+
+
+def packed_scan(T, starts, softplus=True, seed=3):
+    n = Draw(seed)
+    E, N, units = 20, 16, len(starts) - 1
+    i = {"x": n(1, T, E), "dt": n(1, T, E, scale=0.7), "A_log": n(E, N, scale=0.3), "B": n(1, T, 1, N), "C": n(1, T, 1, N),
+         "D": n(E), "z": n(1, T, E), "dt_bias": n(E) if softplus else None, "dt_softplus": softplus,
+         "initial_states": n(units, E, N), "seq_idx": seq_idx_of(starts), "nseq": units}
+    return i, {"dy": n(1, T, E), "dfinal_states": n(units, E, N)}
+
+
+@pytest.mark.parametrize("what", [("dt",), ("z", "B", "C"), ("dy", "dfinal_states"), ("x", "dt", "z", "B", "C", "dy")])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("T,starts", [(40, [0, 5, 9, 40]), (700, [0, 130, 300, 700])])
+def test_an_odd_sequence_of_the_scan_stays_by_itself(T, starts, value, what):
+    """Whatever one packed sequence holds, the others' results keep their bits."""
+    announce("scan: %s in %s of one packed sequence of %d tokens" % (value, what, T))
+    i, back = packed_scan(T, starts)
+
+    def results():
+        y, f = ssd.scan_forward(**i)
+        g = ssd.scan_backward(**i, **back)
+        return [y, g["dx"], g["ddt"], g["dz"], g["dB"], g["dC"]], [f, g["dinit"]]
+
+    clean = results()
+    for k in what:
+        t = {**i, **back}[k]
+        if k == "dfinal_states":
+            t[1] = value
+        else:
+            t[:, starts[1]:starts[2]] = value
+    got = results()
+    for a, c in zip(got[0], clean[0]):
+        assert same(a[:, :starts[1]], c[:, :starts[1]]) and same(a[:, starts[2]:], c[:, starts[2]:])
+    for a, c in zip(got[1], clean[1]):
+        assert same(a[[0, 2]], c[[0, 2]])
+
+
+def test_packed_sequences_that_grow():
+    """Without softplus time steps may be negative and states grow: each of the eleven
+    sequences by up to 2^70 here, which the others do not meet.  (An exponent of 17 is off
+    by 17 roundings, four tokens' by 70: within what check allows.)"""
+    announce("scan: packed sequences with negative time steps")
+    starts = [0, 4, *range(6, 40, 4), 40]     # (tiles of 8 tokens start within sequences)
+    i, back = packed_scan(40, starts, softplus=False)
+    i["dt"].fill_(-0.75)
+    i["A_log"].copy_(torch.log(torch.arange(1, 17).float()).expand(20, 16))
+    spans = mixer.packed(starts)
+    names = {"softplus": False, "init": i["initial_states"], "spans": spans,
+             **{k: i[k] for k in ("x", "dt", "A_log", "B", "C", "D", "z", "dt_bias")}}
+    y, f = ssd.scan_forward(**i)
+    want_y, want_f = mixer.scan_forward(**names)
+    check("y", y, want_y)
+    check("final", f, want_f)
+    g = ssd.scan_backward(**i, **back)
+    want = mixer.scan_backward(**names, dy=back["dy"], dfinal=back["dfinal_states"])
+    for k in ("dx", "ddt", "dz", "dB", "dC", "dA_log", "dD", "dinit"):
+        check(k, g[k], want[k])
