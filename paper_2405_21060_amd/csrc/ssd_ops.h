@@ -124,12 +124,19 @@ __device__ __forceinline__ int64_t held(int32_t id, int64_t nseq)
     return v < nseq ? v : nseq - 1;
 }
 
-// exp(-v): 2^t (1 + r), t = -v log2(e) rounded and r what the rounding left over
-// (where 2^t alone is off by |v| 6e-8); relative error near 2e-7.  v is held to
-// +-104, beyond which the result is infinite or 0; a NaN counts as one of the two.
-// 2^t is infinite from v < -88.7 on and r of either sign, so r is taken of the largest
-// finite number there: infinity times an r of 0 or below would be a NaN, or make one.
-// LARGE: v may be that small (false: a v of 0 and more needs no such care).
+// exp(v) of v in [-104, 88]: 2^t (1 + r), t = v log2(e) rounded and r what the rounding
+// left over (where 2^t alone is off by |v| 6e-8); relative error near 2e-7.
+__device__ __forceinline__ float exp_of(float v)
+{
+    const float t = v * kLog2e, e = __builtin_amdgcn_exp2f(t);
+    return fmaf(e, fmaf(t, -0.69314718f, v), e);
+}
+
+// exp(-v), likewise.  v is held to +-104, beyond which the result is infinite or 0; a
+// NaN counts as one of the two.  2^t is infinite from v < -88.7 on and r of either sign,
+// so r is taken of the largest finite number there: infinity times an r of 0 or below
+// would be a NaN, or make one.  LARGE: v may be that small (false: a v of 0 and more
+// needs no such care).
 template <bool LARGE = true>
 __device__ __forceinline__ float exp_neg(float v)
 {

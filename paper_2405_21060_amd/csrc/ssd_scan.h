@@ -163,8 +163,15 @@ __device__ __forceinline__ void store_states(float* s, const ScanParams& p, int6
     for (int k = 0; k < kSlice / 4; ++k) at[k] = make_float4(h[4 * k], h[4 * k + 1], h[4 * k + 2], h[4 * k + 3]);
 }
 
-// A in log2 units: exp(dt A) = exp2(dt A2).
-__device__ __forceinline__ float decay_rate(float a_log) { return exp_neg(-a_log) * -kLog2e; }
+// A in log2 units: exp(dt A) = exp2(dt A2).  A_log is held to [-104, 88], so that A is
+// finite and a time step of 0 keeps the state, as it does where A = -exp(A_log) is
+// beyond float32; any other step forgets it.  (minimum and maximum, not a median: a NaN
+// stays one.)
+__device__ __forceinline__ float decay_rate(float a_log)
+{
+    const float a = __builtin_elementwise_minimum(__builtin_elementwise_maximum(a_log, -104.f), 88.f);
+    return exp_of(a) * -kLog2e;
+}
 
 __device__ __forceinline__ float time_step(const ScanParams& p, float v) { return p.softplus ? softplus_hw(v) : v; }
 

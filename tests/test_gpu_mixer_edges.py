@@ -141,3 +141,68 @@ def test_packed_sequences_that_grow():
     want = mixer.scan_backward(**names, dy=back["dy"], dfinal=back["dfinal_states"])
     for k in ("dx", "ddt", "dz", "dB", "dC", "dA_log", "dD", "dinit"):
         check(k, g[k], want[k])
+
+
+def test_decay_rates_of_any_size():
+    """A = -exp(A_log) beyond float32 (the state is forgotten, by any time step but 0) and
+    0 (nothing is): no NaN where the definition has none."""
+    announce("scan: A_log from -inf to 1e30")
+    a_log = torch.tensor([float("-inf"), -1e30, -200.0, -104.0, -95.0, 0.0, 1.0, 80.0, 87.0, 88.5, 89.0, 90.0, 93.0, 95.0,
+                          97.0, 104.0, 300.0, 700.0])
+    n, E, T = Draw(7), len(a_log), 40
+    i = {"x": n(2, T, E), "dt": n(2, T, E).abs() + 0.01, "A_log": a_log.cuda()[:, None].repeat(1, 16), "B": n(2, T, 1, 16),
+         "C": n(2, T, 1, 16), "initial_states": n(2, E, 16)}
+    i["dt"][:, ::3] = 0.0
+    names = {"D": None, "z": None, "dt_bias": None, "softplus": False, "init": i["initial_states"], "spans": mixer.rows(2, T),
+             **{k: i[k] for k in ("x", "dt", "A_log", "B", "C")}}
+    y, f = ssd.scan_forward(**i, dt_softplus=False)
+    want_y, want_f = mixer.scan_forward(**names)
+    check("y", y, want_y)
+    check("final", f, want_f)
+    dy, df = n(2, T, E), n(2, E, 16)
+    g, want = ssd.scan_backward(**i, dy=dy, dfinal_states=df, dt_softplus=False), mixer.scan_backward(**names, dy=dy, dfinal=df)
+    for k in ("dx", "dB", "dC", "dinit"):
+        check(k, g[k], want[k])
+    for e, a in enumerate(a_log.tolist()):   # 
+        # ddt holds A itself at the time steps of 0, times up to 10 here: at A_log 87 (A
+        # 6.1e37) the definition's largest is 6.3e38, more than float32 holds (3.4e38)
+        if a <= 80:
+            check("ddt of A_log %g" % a, g["ddt"][..., e], want["ddt"][..., e])
+        if 2 < a:
+            assert torch.all(g["dA_log"][e] == 0), a
+        elif a > -87:
+            check("dA_log of %g" % a, g["dA_log"][e], want["dA_log"][e])
+        else:                                # (A itself is below 2^-126 and may count as 0)
+            assert torch.all(g["dA_log"][e].cpu().double().abs() <= 2 * want["dA_log"][e].abs() + 2.0 ** -126), a
+    state = i["initial_states"].clone()
+    for t in range(4):
+        step = ssd.scan_step(i["x"][:, t], i["dt"][:, t], i["A_log"], i["B"][:, t], i["C"][:, t], state, dt_softplus=False)
+        check("step", step, want_y[:, t])
+
+
+def test_a_decay_rate_that_is_no_number():
+    """A NaN in A_log is a NaN in its channel's results, and in no other's."""
+    announce("scan: NaN in A_log")
+    n, E, T = Draw(7), 70, 300
+    i = {"x": n(1, T, E), "dt": n(1, T, E), "A_log": n(E, 16), "B": n(1, T, 1, 16), "C": n(1, T, 1, 16)}
+    dy = n(1, T, E)
+    state = torch.zeros(1, E, 16).cuda()
+
+    def results():
+        y, f = ssd.scan_forward(**i)
+        g = ssd.scan_backward(**i, dy=dy)
+        s = state.clone()
+        step = ssd.scan_step(i["x"][:, 0], i["dt"][:, 0], i["A_log"], i["B"][:, 0], i["C"][:, 0], s)
+        return {"y": y, "dx": g["dx"], "ddt": g["ddt"], "step": step}, {"f": f, "dA_log": g["dA_log"][None], "s": s}
+
+    clean = results()
+    i["A_log"][3, 5] = float("nan")
+    got = results()
+    others = [e for e in range(E) if e != 3]
+    for k, t in got[0].items():
+        assert same(t[..., others], clean[0][k][..., others]), k
+    for k in ("y", "ddt", "step"):
+        assert torch.isnan(got[0][k][..., 3]).all(), k
+    for k, t in got[1].items():
+        assert same(t[:, others], clean[1][k][:, others]), k
+        assert torch.isnan(t[:, 3, 5]).all(), k
