@@ -550,7 +550,8 @@ int ssd_conv_step(const ssd_conv_problem* prob, const void* x, const float* weig
  *   initial_states, final_states   (batch, channels, dstate) float32, 16-byte
  *                   aligned, contiguous, or NULL; (nseq, ...) with seq_idx
  * dstate is a multiple of 16 in [16, 256].  The states and all arithmetic are
- * float32; a decay below 2^-126 counts as 0.  Outputs must not overlap inputs.  The
+ * float32; a decay below 2^-126 counts as 0, and an A beyond float32 keeps a state over
+ * time steps of 0 alone.  Outputs must not overlap inputs.  The
  * sequence is cut into chunks where its channels alone do not fill the device: their
  * states from zero, a scan over the chunks, then the outputs.  Workspace: ssd_scan_workspace_bytes() (for
  * the forward; may be 0).  Ownership, asynchrony, determinism and errors as for
@@ -608,9 +609,12 @@ int ssd_scan_step(const ssd_scan_problem* prob, const void* x, const void* dt, c
  *   SSD_DTYPE_I8, SSD_DTYPE_E4M3    8-bit values q with a scale per row, y ~ q scale:
  *       t = r weight, m = max |t|, q = (t / m) top rounded to nearest even,
  *       scale = m / sqrt(mean(r^2) + eps) / top, top = 127 (I8) or 448 (E4M3, the
- *       format with no infinities).  A row of zeros has scale 0 and q 0; a row
- *       that holds a NaN or an infinity, or whose squares overflow float32, has
- *       scale NaN and q 0.
+ *       format with no infinities).  A row of zeros has scale 0 and q 0, whatever
+ *       eps is; a row that holds a NaN or an infinity, or whose squares overflow
+ *       float32, has scale NaN and q 0.
+ * With eps = 0 the formula has no value for a row of zeros: its y and gradients are
+ * NaN; nor are those, or the scale, of another row finite whose mean square vanishes in
+ * float32 (|r| < 2^-75).
  * x, residual, y, residual_out are contiguous (rows, channels); x's dtype is
  * `dtype`, the residual's residual_dtype (float32 where x is).  weight (channels)
  * float32.  1 <= channels <= 32768 (else SSD_ERR_UNSUPPORTED_DIMS).  residual_out

@@ -202,8 +202,8 @@ __global__ __launch_bounds__(kWidest) void k_add_norm(NormParams p)
         constexpr float kTop = OUT == kNormI8 ? 127.f : 448.f;
         uint8_t* q = static_cast<uint8_t*>(p.y) + row * p.C;
         const bool bad = !(sum < INFINITY) || !(most < INFINITY);
-        if (lane == 0) p.scale[row] = bad ? __uint_as_float(0x7FC00000u) : most * rstd / kTop;
-        const bool none = bad || most == 0.f;
+        const bool none = bad || most == 0.f;   // (without eps, rstd of a row of zeros is infinite)
+        if (lane == 0) p.scale[row] = bad ? __uint_as_float(0x7FC00000u) : none ? 0.f : most * rstd / kTop;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int c = (k * lanes + lane) * kV;

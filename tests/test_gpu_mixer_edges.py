@@ -206,3 +206,19 @@ def test_a_decay_rate_that_is_no_number():
     for k, t in got[1].items():
         assert same(t[:, others], clean[1][k][:, others]), k
         assert torch.isnan(t[:, 3, 5]).all(), k
+
+
+@pytest.mark.parametrize("to", [torch.int8, torch.float8_e4m3fn])
+@pytest.mark.parametrize("C", [8, 300, 9000])
+def test_rows_of_zeros_without_eps(C, to):
+    announce("add_norm_q8: rows of zeros, eps 0, %d channels" % C)
+    x = Draw(2)(4, C)
+    x[1] = 0.0
+    weight = torch.ones(C).cuda()
+    q, scale, _ = ssd.add_norm_q8(x, weight, eps=0.0, dtype=to)
+    assert scale[1] == 0 and torch.all(q[1].float() == 0)
+    want, _ = mixer.add_norm(x[[0, 2, 3]], weight, None, 0.0)
+    check("scale", scale[[0, 2, 3]], want.abs().amax(-1) / (127.0 if to is torch.int8 else 448.0))
+    weight.zero_()                       # (and t = r w of rows that are not)
+    q, scale, _ = ssd.add_norm_q8(x, weight, eps=0.0, dtype=to)
+    assert torch.all(scale == 0) and torch.all(q.float() == 0)
