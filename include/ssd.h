@@ -550,12 +550,11 @@ int ssd_conv_step(const ssd_conv_problem* prob, const void* x, const float* weig
  *   initial_states, final_states   (batch, channels, dstate) float32, 16-byte
  *                   aligned, contiguous, or NULL; (nseq, ...) with seq_idx
  * dstate is a multiple of 16 in [16, 256].  The states and all arithmetic are
- * float32; a decay below 2^-126 counts as 0, and an A beyond float32 keeps a state over
- * time steps of 0 alone.  Outputs must not overlap inputs.  The
- * sequence is cut into chunks where its channels alone do not fill the device: their
- * states from zero, a scan over the chunks, then the outputs.  Workspace: ssd_scan_workspace_bytes() (for
- * the forward; may be 0).  Ownership, asynchrony, determinism and errors as for
- * ssd_forward. */
+ * float32; a decay below 2^-126 counts as 0, an A_log above 88 as 88.  Outputs must not
+ * overlap inputs.  The sequence is cut into chunks where its channels alone do not fill
+ * the device: their states from zero, a scan over the chunks, then the outputs.
+ * Workspace: ssd_scan_workspace_bytes() (for the forward; may be 0).  Ownership,
+ * asynchrony, determinism and errors as for ssd_forward. */
 typedef struct {
     int64_t batch, seqlen, channels, dstate, ngroups;
     int64_t nseq;                             /* read only when seq_idx != NULL      */

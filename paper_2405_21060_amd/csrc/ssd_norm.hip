@@ -257,7 +257,8 @@ struct GradValues {
 // lane the weights stay in registers too, and the next row is loaded before the
 // present one's sums are joined; a wider row has no registers for that and is read
 // once more, from the cache, after its sums (16,384 x 20,000 bf16 637 us, kept in
-// registers, which spill, 1,590).
+// registers 1,590).  Above 16,384 channels, with 32 sums of dweight a lane, that still
+// leaves 2 to 67 values of a lane in scratch memory.
 template <typename T, typename R, int NV, bool WHOLE>
 __global__ __launch_bounds__(kWidest) void k_add_norm_backward(NormParams p, int64_t step)
 {

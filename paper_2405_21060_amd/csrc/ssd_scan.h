@@ -165,7 +165,7 @@ __device__ __forceinline__ void store_states(float* s, const ScanParams& p, int6
 
 // A in log2 units: exp(dt A) = exp2(dt A2).  A_log is held to [-104, 88], so that A is
 // finite and a time step of 0 keeps the state, as it does where A = -exp(A_log) is
-// beyond float32; any other step forgets it.  (minimum and maximum, not a median: a NaN
+// beyond float32; a step above 1e-36 forgets it.  (minimum and maximum, not a median: a NaN
 // stays one.)
 __device__ __forceinline__ float decay_rate(float a_log)
 {

@@ -16,11 +16,11 @@
 // (k_scan_chunk<kOutputReady>); the first of the three costs five more slots.
 // Sequences of a packed row replace the state at their first token.
 //
-// Measured (bf16, gate): 4 x 4,096 x 5,120 505 us, the output pass 300 of them, the
+// Measured (bf16, gate): 4 x 4,096 x 5,120 508 us, the output pass 300 of them, the
 // states 240 (traced alone each a little slower); one pass over the tokens needs
-// 205 at one slot a cycle and 2.4 GHz, its bytes 132.  1 x 65,536 x 1,536 640 us
-// (358, 287 and 57 for the scan over 410 chunks).  The vector units are busy 98 % of
-// the chunk kernels' time.
+// 205 at one slot a cycle and 2.4 GHz, its bytes 132.  1 x 65,536 x 1,536 646 us
+// (351, 281 and 57 for the scan over 410 chunks, each alone).  The vector units are busy
+// 98 % of the chunk kernels' time.
 #include <type_traits>
 
 #include "ssd_internal.h"
@@ -40,7 +40,8 @@ enum Mode { kOutput, kOutputReady, kStates, kBoth };
 // both), and in front of every tile of kBwdTile tokens the state, from zero as it
 // is, and the sum of dt since the chunk's start.
 // Workgroup: a wavefront per 16 states, at most THREADS / 64 of them (the bound
-// says how many registers a lane may have).
+// says how many registers a lane may have; with more than 64 states kBoth does not fit
+// them, up to 45 values of a lane are in scratch memory).
 //
 // A tile is kTok tokens; the next one's are loaded, and its B and C a token ahead,
 // before they are needed.  With several wavefronts their shares of y meet in shared

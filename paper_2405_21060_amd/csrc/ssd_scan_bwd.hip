@@ -20,11 +20,16 @@
 // where a sum of its own would take seven.  Sums over channel tiles, chunks and
 // rows are joined in a fixed order by k_scan_sum_params and k_scan_sum_bc.
 //
-// Bound by vector arithmetic, like the forward: 8 x 2,048 x 1,536 bf16 with a gate 548
-// us, of which k_scan_grad 405, where the vector units are busy 72 % of the time (two
+// Bound by vector arithmetic, like the forward: 8 x 2,048 x 1,536 bf16 with a gate 546
+// us, of which k_scan_grad 404, where the vector units are busy 72 % of the time (two
 // wavefronts a SIMD: a tile's states and decays fill the registers), k_scan_chunk<kBoth>
-// 131.  The states of every token written out by the first pass and read again, in
-// place of computing them twice, would move 3.2 GB, 630 us at a copy's rate.
+// 131.  The scalars do not fit their registers either (row pointers, B and C of a tile's
+// tokens): of 3,290 vector instructions a tile 240 move them to and from lanes.  For
+// packed rows, where every tile asks for sequence edges, the round of four states has
+// 1,468 instructions, 299 of those moves, instead of 660: 1 x 16,384 tokens x 1,536 868
+// us, k_scan_grad 490 and the scans over chunks 203 (not packed 597).  The states of
+// every token written out by the first pass and read again, in place of computing them
+// twice, would move 3.2 GB (8 x 2,048 x 1,536), 630 us at a copy's rate.
 #include <type_traits>
 
 #include "ssd_internal.h"
